@@ -218,6 +218,116 @@ int covspec_correct(int logit_dtype, int rows, int vocab, long long ld, const vo
                     float* margin, int* gate, float* accept, float* resid_mass, int* token,
                     void* stream);
 
+/* ---- The verification of drafted blocks around covspec_correct: a paged cache of keys and values, attention over it, and
+ * edits of the logits.  (The paper runs the target model's verification in its serving framework; these are the operators of
+ * that step.)  None of these calls needs a context; they allocate nothing, wait for nothing and may be captured.  All arrays
+ * that are not called host lie on the current device.  Offsets, lengths and page ids are read on the device: values that make
+ * no sense never lead outside the arrays given here (each entry says what happens instead). ---- */
+
+/* A paged cache of one layer.  A page holds page_size positions of all key heads: [heads, page_size, head_dim], dense, pages
+ * k_page_stride (v_page_stride) elements apart, so keys and values may be halves of one array.  Bases and strides are multiples
+ * of 16 bytes.
+ * store: COVSPEC_F32, COVSPEC_BF16, COVSPEC_F16: rows as they are; COVSPEC_E4M3, COVSPEC_INT8: one byte a value and a float32
+ * scale for each position and head, [pages, heads, page_size] dense.  A row x is held as x / scale, rounded once, half to even,
+ * from the exact quotient, with scale = max(max|x| / L, 2^-100) in float32 and L = 448 or 127.  A row with a value that is not
+ * finite gets the scale NaN, which makes everything that reads it NaN.  The codes of NaN (e4m3) and -128 (int8) are not
+ * written; a cache from elsewhere must not hold the former. */
+#define COVSPEC_E4M3 3
+#define COVSPEC_INT8 4
+typedef struct {
+  int store;
+  int pages, heads;
+  int page_size;               /* positions in a page: a power of two, at most 4096                */
+  int head_dim;                /* 64 or 128                                                        */
+  void* k;
+  void* v;
+  float* k_scale;              /* 8-bit stores only                                                */
+  float* v_scale;
+  long long k_page_stride, v_page_stride;
+} covspec_cache;
+
+/* The tokens of a call, packed request by request: request b owns tokens offsets[b] .. offsets[b+1] - 1, which are the last
+ * ones of its lengths[b] positions (token i of n has position lengths[b] - n + i).  Position t lies in page
+ * table[b * table_stride + t / page_size].  Positions below 0 or past the table, and page ids outside the cache, have no place:
+ * nothing is written there, zeros are read back, and their keys are not attended to.  Tokens of no request (before offsets[0],
+ * from offsets[batch] on) are left alone, and so are the outputs' rows of them. */
+typedef struct {
+  int batch;
+  const int* offsets;          /* device [batch + 1], ascending                                    */
+  const int* lengths;          /* device [batch]: positions in the cache, the call's tokens among them */
+  const int* table;            /* device [batch, table_stride]                                     */
+  int table_width;             /* page ids per request                                             */
+  long long table_stride;
+} covspec_tokens;
+
+/* Writes the keys and values of `n` tokens.
+ *  dtype         of k and v: COVSPEC_F32, COVSPEC_BF16 or COVSPEC_F16; any store
+ *  k, v          device rows [heads, head_dim], dense, k_stride (v_stride) elements apart; bases and strides multiples of 16 bytes
+ *  rows          device [n] or NULL: token i of request b is row row_offsets[b] + rows[i] of k and v instead of row i.  With the
+ *                keep_idx of covspec_select and the vis_offsets (on the device) the kept tokens' rows of a prefill go into the
+ *                cache without a dense copy between.  Rows outside 0 .. source_rows - 1 are not written
+ *  row_offsets   device [batch + 1]; with rows only
+ *  source_rows   rows that k and v have (without rows: at least n)
+ * Two tokens of one call must not share a place. */
+int covspec_cache_write(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* k, const void* v,
+                        long long k_stride, long long v_stride, const int* rows, const int* row_offsets, int source_rows,
+                        void* stream);
+
+/* Reads the keys and values of `n` tokens back as dense rows [n, heads, head_dim] of `dtype` (8-bit stores: value * scale,
+ * rounded once).  With offsets that are the prefix sums of the lengths, whole caches. */
+int covspec_cache_read(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, void* k, void* v, void* stream);
+
+/* Attention of the call's tokens over the cache, which already holds them (covspec_cache_write).  The token at position p
+ * attends to the positions max(0, p - window + 1) .. p of its request: o = sum_j softmax_j(scale q . k_j) v_j.  Query head h
+ * reads key head h / (q_heads / heads).  Probabilities are rounded to dtype before the second product; scores, maxima, sums and
+ * accumulators are float32.  A token without a key (a position below 0) gets zeros and the sum -inf.  What the cache holds past
+ * a request's length is never read; the values of its positions that a token may not see have to be finite where another token
+ * of the call may see them.
+ *  dtype         of q and out: COVSPEC_BF16 or COVSPEC_F16; the cache's store is the same or an 8-bit one
+ *  q, out        device [n] rows [q_heads, head_dim], dense, q_stride (out_stride) elements apart; multiples of 16 bytes
+ *  q_heads       a multiple of the cache's heads
+ *  window        0: none
+ *  max_new       most tokens of a request, or 0: unknown.  A hint for the choice of the kernels: results do not depend on it
+ *  lse           device [n, q_heads] float32 or NULL (out): log of the sum of exp(scale q . k_j)
+ *  workspace     device, covspec_cache_attend_workspace(...) bytes, 16-byte aligned; contents do not matter.  Calls that may
+ *                overlap on the GPU need workspaces of their own
+ * Results are deterministic, and how the work was split shows in the last bits only. */
+int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
+                         long long q_stride, int q_heads, float scale, int window, int max_new, void* out, long long out_stride,
+                         float* lse, void* workspace, long long workspace_bytes, void* stream);
+/* Bytes that covspec_cache_attend needs on the current device for these arguments; a negative status for bad ones.  Grows
+ * neither with the lengths nor with n. */
+long long covspec_cache_attend_workspace(const covspec_cache* cache, int q_heads);
+
+/* Edits of logits: penalties for repeated tokens, biases, masks of a grammar.  Any pointer may be NULL (no such edit), but
+ * row_offsets, and what belongs to a list that is given.  All arrays on the device. */
+typedef struct {
+  int batch;
+  const int* row_offsets;      /* [batch + 1]: request b owns rows row_offsets[b] .. row_offsets[b+1] - 1, the positions of its
+                                  drafted block in order; rows of no request are left as they were                    */
+  const int* history;          /* token ids of all requests; ids outside the vocabulary are passed over               */
+  const int* history_offsets;  /* [batch + 1]                                                                        */
+  int history_len;             /* elements of history                                                                */
+  const int* prompt_lengths;   /* [batch]: the first ones of a request's history that are its prompt; NULL: none      */
+  const int* drafted;          /* [rows] token drafted at each row: part of the history of the later rows of its block */
+  const float* repetition;     /* [batch] r > 0: a logit x of a token in the history becomes x / r (x > 0) or x * r    */
+  const float* presence;       /* [batch] taken off once where the token occurs after the prompt                      */
+  const float* frequency;      /* [batch] taken off for each occurrence after the prompt                              */
+  const int* bias_ids;         /* token ids of all requests with ...                                                 */
+  const float* bias_values;    /* ... what is added to their logits; of an id given twice the later one counts         */
+  const int* bias_offsets;     /* [batch + 1]                                                                        */
+  int bias_len;                /* elements of bias_ids and bias_values                                               */
+  const void* mask;            /* [rows] of mask_stride bytes: bit w % 8 of byte w / 8 says that token w is allowed (int32
+                                  words on this machine: bit w % 32 of word w / 32); others become -inf               */
+  long long mask_stride;       /* at least (vocab + 7) / 8                                                           */
+} covspec_edits;
+
+/* z -> out, both [rows, ld] of `logit_dtype`, laid out and aligned as in covspec_correct; out may be z itself, or must not
+ * overlap it.  In order: repetition, frequency, presence, bias, mask; float32 arithmetic, rounded once.  Entries that no edit
+ * concerns keep their bits; columns from vocab on are not written. */
+int covspec_edit_logits(int logit_dtype, int rows, int vocab, long long ld, const void* z, void* out, const covspec_edits* edits,
+                        void* stream);
+
 /* Fan-out of the parallel branching, Eq. 23: F_j = ceil(F_0 * rho^j), 0 < rho < 1, evaluated in
  * double (a product within 1e-9 of an integer counts as that integer).  Host only. */
 int covspec_fanout(int f0, double rho, int j);

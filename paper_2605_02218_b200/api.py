@@ -20,7 +20,7 @@ import torch
 _LIB_PATH = os.environ.get("COVSPEC_LIBRARY") or \
     os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcovspec.so")
 
-COVSPEC_F32, COVSPEC_BF16, COVSPEC_F16 = 0, 1, 2
+COVSPEC_F32, COVSPEC_BF16, COVSPEC_F16, COVSPEC_E4M3, COVSPEC_INT8 = 0, 1, 2, 3, 4
 NORM_MODES = {"minmax": 0, "zscore": 1, "none": 2}
 HEAD_REDUCE = {"max": 0, "mean": 1}
 
@@ -35,6 +35,8 @@ EXPORTS = [
     "covspec_uplink_bits", "covspec_downlink_bits", "covspec_comm_latency", "covspec_ema_update",
     "covspec_draft_length", "covspec_get_iteration_counts", "covspec_build_has_bounds_checks",
     "covspec_selftest_fill_workspace", "covspec_selftest_static_timeout",
+    "covspec_cache_write", "covspec_cache_read", "covspec_cache_attend", "covspec_cache_attend_workspace",
+    "covspec_edit_logits",
 ]
 STATIC_MAX_BATCH = 256
 STATIC_MAX_QUERY_ELEMS = 1 << 20
@@ -60,6 +62,30 @@ class Problem(C.Structure):
         ("Q", C.c_void_p), ("txt_offsets", C.POINTER(C.c_int)), ("Wq", C.c_void_p),
         ("Wk", C.c_void_p), ("Hs", C.POINTER(C.c_void_p)), ("keep", C.POINTER(C.c_int)),
         ("keep_ratio", C.c_double),
+    ]
+
+
+class Cache(C.Structure):
+    _fields_ = [
+        ("store", C.c_int), ("pages", C.c_int), ("heads", C.c_int), ("page_size", C.c_int), ("head_dim", C.c_int),
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("k_page_stride", C.c_longlong), ("v_page_stride", C.c_longlong),
+    ]
+
+
+class Tokens(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int), ("offsets", C.c_void_p), ("lengths", C.c_void_p), ("table", C.c_void_p),
+        ("table_width", C.c_int), ("table_stride", C.c_longlong),
+    ]
+
+
+class Edits(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int), ("row_offsets", C.c_void_p), ("history", C.c_void_p), ("history_offsets", C.c_void_p),
+        ("history_len", C.c_int), ("prompt_lengths", C.c_void_p), ("drafted", C.c_void_p), ("repetition", C.c_void_p),
+        ("presence", C.c_void_p), ("frequency", C.c_void_p), ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p),
+        ("bias_offsets", C.c_void_p), ("bias_len", C.c_int), ("mask", C.c_void_p), ("mask_stride", C.c_longlong),
     ]
 
 
@@ -130,6 +156,14 @@ def load_library():
     lib.covspec_profile_stage_count.argtypes = []
     lib.covspec_profile_stage_name.argtypes = [C.c_int]
     lib.covspec_profile_stage_name.restype = C.c_char_p
+    cp, tp, ll = C.POINTER(Cache), C.POINTER(Tokens), C.c_longlong
+    lib.covspec_cache_write.argtypes = [cp, tp, C.c_int, C.c_int, vp, vp, ll, ll, vp, vp, C.c_int, vp]
+    lib.covspec_cache_read.argtypes = [cp, tp, C.c_int, C.c_int, vp, vp, vp]
+    lib.covspec_cache_attend.argtypes = [cp, tp, C.c_int, C.c_int, vp, ll, C.c_int, C.c_float, C.c_int, C.c_int, vp, ll, vp, vp,
+                                         ll, vp]
+    lib.covspec_cache_attend_workspace.argtypes = [cp, C.c_int]
+    lib.covspec_cache_attend_workspace.restype = ll
+    lib.covspec_edit_logits.argtypes = [C.c_int, C.c_int, C.c_int, ll, vp, vp, C.POINTER(Edits), vp]
     from .build import binding_path
     _native = _load_native(lib, binding_path())
     _lib = lib
@@ -564,3 +598,211 @@ def branch_candidates(z_draft: torch.Tensor, fanouts, drafted: Optional[torch.Te
     if st:
         raise CovspecError(st, "covspec_branch_candidates")
     return (cand if total else cand[:0]), off
+
+
+_STORES = {torch.float32: COVSPEC_F32, torch.bfloat16: COVSPEC_BF16, torch.float16: COVSPEC_F16,
+           torch.float8_e4m3fn: COVSPEC_E4M3, torch.int8: COVSPEC_INT8}
+
+
+def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, device: torch.device, heads: int, head_dim: int):
+    """(address, stride) of rows [n, heads, head_dim] that are dense but for the step from row to row."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: a tensor is required, not {type(t).__name__}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: {dtype} is required, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the call is on {device}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, [tokens, {heads}, {head_dim}] is required")
+    if t.shape[0] and not t[0].is_contiguous():
+        raise ValueError(f"{name}: rows have to be dense")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * head_dim
+
+
+class PagedCache:
+    """Keys and values of one layer in pages (covspec_cache): `k`, `v` [pages, heads, page_size, head_dim] in float32,
+    bfloat16, float16, float8_e4m3fn or int8, each page dense; the two 8-bit types come with `k_scale`, `v_scale` [pages, heads,
+    page_size] float32.  The tensors stay the caller's: `k` and `v` may be views of one allocation.
+
+    The calls take the tokens of a batch, packed request by request: `offsets` [batch + 1], `lengths` [batch] and `table` [batch,
+    pages of a request], int32 on the cache's device.  Request b's tokens offsets[b] .. offsets[b+1] are the last ones of its
+    lengths[b] positions."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        if not (isinstance(k, torch.Tensor) and isinstance(v, torch.Tensor)) or k.dtype not in _STORES or v.dtype != k.dtype:
+            raise TypeError("k, v: tensors of one type are required, float32, bfloat16, float16, float8_e4m3fn or int8")
+        if not k.is_cuda or v.device != k.device:
+            raise ValueError(f"k on {k.device}, v on {v.device}: one CUDA device is required")
+        if k.dim() != 4 or v.shape != k.shape:
+            raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}: [pages, heads, page_size, head_dim] is required of both")
+        for name, t in (("k", k), ("v", v)):
+            if not t.numel() or not t[0].is_contiguous():
+                raise ValueError(f"{name}: dense pages are required")
+        store, page = _STORES[k.dtype], k[0].numel()
+        scales = (k_scale, v_scale)
+        if (store >= COVSPEC_E4M3) != all(s is not None for s in scales) or (store < COVSPEC_E4M3 and any(s is not None for s in scales)):
+            raise ValueError("k_scale, v_scale: required of the 8-bit types and of no other")
+        pages, heads, page_size, head_dim = k.shape
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._c = Cache(store, _c_int(pages, "pages"), _c_int(heads, "heads"), _c_int(page_size, "page_size"), head_dim,
+                        k.data_ptr(), v.data_ptr(),
+                        *(_addr(s, n, torch.float32, k.device, pages * heads * page_size)
+                          for n, s in (("k_scale", k_scale), ("v_scale", v_scale))),
+                        *(t.stride(0) if pages > 1 else page for t in (k, v)))
+        self._ref = C.byref(self._c)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, dtype: torch.dtype, device="cuda") -> "PagedCache":
+        """A cache in memory of its own; what it holds is undefined until it is written."""
+        k, v = (torch.empty(pages, heads, page_size, head_dim, dtype=dtype, device=device) for _ in range(2))
+        if _STORES.get(dtype, -1) < COVSPEC_E4M3:
+            return cls(k, v)
+        return cls(k, v, *(torch.empty(pages, heads, page_size, dtype=torch.float32, device=device) for _ in range(2)))
+
+    def _tokens(self, offsets, lengths, table) -> Tokens:
+        dev = self.k.device
+        for name, t, dims in (("offsets", offsets, 1), ("lengths", lengths, 1), ("table", table, 2)):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name}: a tensor is required, not {type(t).__name__}")
+            if t.dim() != dims:
+                raise ValueError(f"{name}: {dims} dimensions are required")
+        batch = lengths.shape[0]
+        if table.shape[0] < batch or table.stride(1) != 1 or (batch > 1 and table.stride(0) < table.shape[1]):
+            raise ValueError(f"table: rows of page ids of {batch} requests are required")
+        if table.dtype != torch.int32:
+            raise TypeError(f"table: {torch.int32} is required, not {table.dtype}")
+        if table.device != dev:
+            raise ValueError(f"table: on {table.device}, the call is on {dev}")
+        return Tokens(_c_int(batch, "batch"), _addr(offsets, "offsets", torch.int32, dev, batch + 1),
+                      _addr(lengths, "lengths", torch.int32, dev, batch), table.data_ptr(), _c_int(table.shape[1], "table"),
+                      max(table.stride(0), table.shape[1]))
+
+    def write(self, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
+              rows: Optional[torch.Tensor] = None, row_offsets: Optional[torch.Tensor] = None) -> None:
+        """covspec_cache_write: keys and values [tokens, heads, head_dim] (float32, bfloat16 or float16; rows may be columns of
+        one projection) into the cache.  With `rows` and `row_offsets` token i of request b is row row_offsets[b] + rows[i]:
+        Pruner.select's keep_idx and the visual offsets (int32, on the device) write the kept tokens of a prefill."""
+        lib, dev = _lib or load_library(), self.k.device
+        dtype = k.dtype if isinstance(k, torch.Tensor) else None
+        if dtype not in _LOGIT_DTYPES:
+            raise TypeError(f"k: float32, bfloat16 or float16 is required, not {dtype}")
+        heads, dim = self._c.heads, self._c.head_dim
+        kp, ks = _rows(k, "k", dtype, dev, heads, dim)
+        vp, vs = _rows(v, "v", dtype, dev, heads, dim)
+        if k.shape[0] != v.shape[0]:
+            raise ValueError(f"k, v: {k.shape[0]} and {v.shape[0]} tokens")
+        tokens = self._tokens(offsets, lengths, table)
+        if (rows is None) != (row_offsets is None):
+            raise ValueError("rows, row_offsets: both or neither")
+        n = k.shape[0] if rows is None else rows.numel()
+        rp, rop = _addr(rows, "rows", torch.int32, dev, n), _addr(row_offsets, "row_offsets", torch.int32, dev, tokens.batch + 1)
+        with torch.cuda.device(dev):
+            st = lib.covspec_cache_write(self._ref, C.byref(tokens), _LOGIT_DTYPES[dtype], _c_int(n, "tokens"), kp, vp, ks, vs, rp, rop,
+                                         _c_int(k.shape[0], "rows of k"), _stream())
+        if st:
+            raise CovspecError(st, "covspec_cache_write")
+
+    def read(self, offsets: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, n: int, dtype: torch.dtype = torch.bfloat16):
+        """covspec_cache_read: (k, v), [n, heads, head_dim] each, of the `n` tokens that `offsets` delimits; rows of no request
+        are undefined."""
+        lib, dev = _lib or load_library(), self.k.device
+        tokens = self._tokens(offsets, lengths, table)
+        if dtype not in _LOGIT_DTYPES:
+            raise TypeError(f"dtype: float32, bfloat16 or float16 is required, not {dtype}")
+        k, v = (torch.empty(n, self._c.heads, self._c.head_dim, dtype=dtype, device=dev) for _ in range(2))
+        with torch.cuda.device(dev):
+            st = lib.covspec_cache_read(self._ref, C.byref(tokens), _LOGIT_DTYPES[dtype], _c_int(n, "n"), k.data_ptr(), v.data_ptr(),
+                                        _stream())
+        if st:
+            raise CovspecError(st, "covspec_cache_read")
+        return k, v
+
+    def attend(self, q: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
+               scale: Optional[float] = None, window: int = 0, max_new: int = 0, lse: bool = False,
+               out: Optional[torch.Tensor] = None):
+        """covspec_cache_attend: attention of the tokens' queries [tokens, q_heads, head_dim] (bfloat16 or float16) over the
+        cache, which already holds their keys and values.  `scale`: 1 / sqrt(head_dim) if None; `window`: positions a token
+        sees, itself among them, 0 for all; `max_new`: most tokens of a request, where the caller knows it (a hint).  Returns
+        the rows (in `out` if given), with `lse` also the float32 log-sums [tokens, q_heads].  Rows of no request are undefined,
+        in a given `out` they are left as they were."""
+        lib, dev = _lib or load_library(), self.k.device
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise ValueError("q: [tokens, q_heads, head_dim] is required")
+        dtype = q.dtype
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"q: bfloat16 or float16 is required, not {dtype}")
+        n, heads = q.shape[0], q.shape[1]
+        qp, qs = _rows(q, "q", dtype, dev, heads, self._c.head_dim)
+        tokens = self._tokens(offsets, lengths, table)
+        if out is None:
+            out = torch.empty(n, heads, self._c.head_dim, dtype=dtype, device=dev)
+        op, os_ = _rows(out, "out", dtype, dev, heads, self._c.head_dim)
+        if out.shape[0] < n:
+            raise ValueError(f"out: {out.shape[0]} rows, {n} are written")
+        logs = torch.empty(n, heads, dtype=torch.float32, device=dev) if lse else None
+        with torch.cuda.device(dev):
+            size = lib.covspec_cache_attend_workspace(self._ref, _c_int(heads, "q_heads"))
+            if size < 0:
+                raise CovspecError(int(size), "covspec_cache_attend")
+            # from torch's pool, like the outputs: it knows streams and captures, so no two calls in flight share it
+            work = torch.empty(size, dtype=torch.uint8, device=dev)
+            st = lib.covspec_cache_attend(self._ref, C.byref(tokens), _LOGIT_DTYPES[dtype], _c_int(n, "tokens"), qp, qs, heads,
+                                          float(scale) if scale is not None else self._c.head_dim ** -0.5, _c_int(window, "window"),
+                                          _c_int(max_new, "max_new"), op, os_, _ptr(logs), work.data_ptr(), size, _stream())
+        if st:
+            raise CovspecError(st, "covspec_cache_attend")
+        return (out, logs) if lse else out
+
+
+def edit_logits(z: torch.Tensor, row_offsets: torch.Tensor, *, history: Optional[torch.Tensor] = None,
+                history_offsets: Optional[torch.Tensor] = None, prompt_lengths: Optional[torch.Tensor] = None,
+                drafted: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                presence: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                bias_ids: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
+                bias_offsets: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                vocab: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """covspec_edit_logits: repetition, frequency and presence penalties, biases and a grammar's mask on the logits [rows, ld] of
+    drafted blocks, before `correct` or `branch_candidates`.  `row_offsets` [batch + 1] delimits the requests' rows; row j of a
+    request counts the tokens `drafted` at its rows before j as history.  `mask`: int32 [rows, ceil(vocab / 32)], bit w % 32 of
+    word w / 32 allows token w.  Everything on z's device, ids and offsets int32, factors float32.  Returns the edited logits (in
+    `out` if given, which may be z); rows of no request and columns past the vocabulary are undefined, or left as they were."""
+    lib = _lib or load_library()
+    if not isinstance(z, torch.Tensor) or z.dim() != 2 or z.dtype not in _LOGIT_DTYPES:
+        raise TypeError("z: a matrix of float32, bfloat16 or float16 is required")
+    if not z.is_cuda:
+        raise ValueError(f"z: on {z.device}, a CUDA device is required")
+    rows, ld = z.shape
+    dev = z.device
+    zp = _addr(z, "z", z.dtype, dev, 0)
+    vocab = ld if vocab is None else _c_int(vocab, "vocab")
+    if out is None:
+        out = torch.empty_like(z)
+    elif isinstance(out, torch.Tensor) and out.shape != z.shape:
+        raise ValueError(f"out: shape {tuple(out.shape)}, z has {tuple(z.shape)}")
+    if not isinstance(row_offsets, torch.Tensor) or row_offsets.numel() < 2:
+        raise ValueError("row_offsets: a tensor of one more than requests is required")
+    batch, i32, f32 = row_offsets.numel() - 1, torch.int32, torch.float32
+    if (history is None) != (history_offsets is None):
+        raise ValueError("history, history_offsets: both or neither")
+    if len({bias_ids is None, bias_values is None, bias_offsets is None}) > 1:
+        raise ValueError("bias_ids, bias_values, bias_offsets: all or none")
+    n_hist, n_bias = 0 if history is None else history.numel(), 0 if bias_ids is None else bias_ids.numel()
+    e = Edits(_c_int(batch, "batch"), _addr(row_offsets, "row_offsets", i32, dev, batch + 1), _addr(history, "history", i32, dev, 0),
+              _addr(history_offsets, "history_offsets", i32, dev, batch + 1), _c_int(n_hist, "history"),
+              _addr(prompt_lengths, "prompt_lengths", i32, dev, batch), _addr(drafted, "drafted", i32, dev, rows),
+              _addr(repetition, "repetition", f32, dev, batch), _addr(presence, "presence", f32, dev, batch),
+              _addr(frequency, "frequency", f32, dev, batch), _addr(bias_ids, "bias_ids", i32, dev, 0),
+              _addr(bias_values, "bias_values", f32, dev, n_bias), _addr(bias_offsets, "bias_offsets", i32, dev, batch + 1),
+              _c_int(n_bias, "bias_ids"))
+    if mask is not None:
+        words = (vocab + 31) // 32
+        if not isinstance(mask, torch.Tensor) or mask.dim() != 2 or mask.shape[0] < rows or mask.shape[1] < words:
+            raise ValueError(f"mask: at least [{rows}, {words}] is required")
+        e.mask, e.mask_stride = _addr(mask, "mask", i32, dev, rows * words), 4 * mask.shape[1]
+    op = _addr(out, "out", z.dtype, dev, z.numel())
+    with torch.cuda.device(dev):
+        st = lib.covspec_edit_logits(_LOGIT_DTYPES[z.dtype], _c_int(rows, "rows"), vocab, ld, zp, op, C.byref(e), _stream())
+    if st:
+        raise CovspecError(st, "covspec_edit_logits")
+    return out

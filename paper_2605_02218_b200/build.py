@@ -3,6 +3,7 @@ is a plain C ABI loaded through ctypes), and the native part of the Python bindi
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
 import sysconfig
@@ -12,12 +13,27 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcovspec.so")
 LIB_DEBUG = os.path.join(HERE, "libcovspec_debug.so")     # the same sources with -DCOVSPEC_DEBUG_BOUNDS
-SOURCES = ["covspec.cu"]
+OBJECTS = os.path.join(HERE, "_build")                    # a compiled source is used again until one of its files changes
+SOURCES = ["covspec.cu", "verify.cu"]
 BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
 
 
 def _newest(paths):
     return max(os.path.getmtime(p) for p in paths)
+
+
+def _files_of(source: str) -> list:
+    """The source and what it includes of this library."""
+    found, todo = [], [source]
+    while todo:
+        path = todo.pop()
+        if path in found:
+            continue
+        found.append(path)
+        with open(path) as f:
+            names = re.findall(r'^\s*#include "([^"]+)"', f.read(), re.M)
+        todo += [p for n in names for p in (os.path.join(CSRC, n), os.path.join(ROOT, "include", n)) if os.path.exists(p)]
+    return found
 
 
 def binding_path() -> str:
@@ -49,21 +65,38 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
     if not force and not needs_build(LIB):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-shared", "-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo",
-           "-gencode", "arch=compute_100a,code=sm_100a",
-           "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
+    target = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    common = [nvcc, "-c", "-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo", *target,
+              "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if debug_bounds:
-        cmd.insert(1, "-DCOVSPEC_DEBUG_BOUNDS")
+        common.append("-DCOVSPEC_DEBUG_BOUNDS")
     if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
+        common += ["-Xptxas", "-v"]
+    os.makedirs(OBJECTS, exist_ok=True)
+    objects, running = [], []
+    for name in SOURCES:
+        source = os.path.join(CSRC, name)
+        objects.append(os.path.join(OBJECTS, os.path.splitext(name)[0] + ("_debug.o" if debug_bounds else ".o")))
+        if force or not os.path.exists(objects[-1]) or _newest(_files_of(source)) > os.path.getmtime(objects[-1]):
+            # under a name of its own until it is whole: what is there later is complete
+            part = f"{objects[-1]}.{os.getpid()}.part"
+            running.append((objects[-1], part, subprocess.Popen([*common, "-o", part, source], stdout=subprocess.PIPE,
+                                                                stderr=subprocess.STDOUT, text=True)))
+    failed = False
+    for path, part, job in running:
+        said = job.communicate()[0]
+        failed |= job.returncode != 0
+        if job.returncode or verbose:
+            sys.stderr.write(said)
+        if not job.returncode:
+            os.replace(part, path)
+    if not failed:
+        res = subprocess.run([nvcc, "-shared", "-Xcompiler", "-fPIC", *target, "-o", LIB, *objects], capture_output=True, text=True)
+        failed = res.returncode != 0
+        if failed:
+            sys.stderr.write(res.stdout + res.stderr)
+    if failed:
         raise RuntimeError("nvcc failed building " + os.path.basename(LIB))
-    if verbose:
-        sys.stderr.write(res.stderr)
     return LIB
 
 

@@ -1,0 +1,225 @@
+// Attention of each request's newest tokens over its paged cache: what the kernels share.
+//
+// Query token i of n of request b stands at position p = length - n + i and attends to the keys max(0, p - window + 1) .. p.
+// The group = q_heads / heads query heads of a key head are rows of one tile: row r of a request is token r / group, query head
+// h * group + r % group.  A key head's rows are cut into items of `tile_rows` rows, an item's keys into units of `tile_keys`;
+// the units of all items, request by request and head by head, form one sequence that the CTAs cut into equal shares, so the
+// split follows the lengths on the device and needs no plan from the host.  An item that lies in one share is finished there.
+// The others leave their running maxima, sums and unnormalised rows in the workspace, and attend_join_kernel adds them up in the
+// order of the shares.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "cache_kernels.cuh"
+#include "tc_common.cuh"
+
+namespace covspec {
+namespace attend {
+
+struct Params {
+  cache::Pages c;
+  cache::Tokens t;
+  const void* q;
+  void* out;
+  float* lse;                    // or null
+  long long q_ld, out_ld;        // elements from token to token
+  int n, q_heads, group, window; // window 0: none
+  float scale_log2;              // scale * log2(e)
+  int rows_over, rows_upto;      // the requests that this launch takes: rows_over < n_b * group <= rows_upto
+  int least_units;               // a share is no smaller
+  float* part;                   // [2 * grid][tile_rows * (dim + 2)]: rows, maxima, sums of the shares' first and last item
+  int4* open;                    // [grid][2]: the item that a share leaves unfinished: first token of its request, head, first
+                                 // row, rows; last share of the item
+};
+
+// One request as the kernels see it.  Offsets, lengths and positions that make no sense give it no rows or no keys.
+struct Request {
+  int q0, n, length, keys, rows;
+};
+__device__ __forceinline__ Request load_request(const Params& p, int b) {
+  Request r;
+  const int a = p.t.offsets[b], e = p.t.offsets[b + 1];
+  r.q0 = max(a, 0);
+  r.n = max(min(e, p.n) - r.q0, 0);
+  r.length = max(p.t.lengths[b], 0);
+  // positions count from the call's own tokens: the ones in front of a cut-off start keep theirs
+  r.keys = (int)min((long long)r.length, (long long)p.t.width << p.c.page_shift);
+  r.rows = r.n * p.group;
+  if (r.rows <= p.rows_over || r.rows > p.rows_upto) r.rows = 0;
+  return r;
+}
+struct Range { int lo, hi; };    // keys lo .. hi - 1
+template <int ROWS>
+__device__ __forceinline__ Range keys_of(const Params& p, const Request& r, int tile) {
+  const int first = tile * ROWS / p.group, last = min((tile + 1) * ROWS, r.rows) - 1;
+  const int end = r.length - r.n + last / p.group + 1;
+  Range k;
+  k.hi = min(max(end, 0), r.keys);
+  k.lo = p.window ? max(r.length - r.n + first - p.window + 1, 0) : 0;
+  return k;
+}
+template <int KEYS>
+__device__ __forceinline__ int units_of(const Range& k) {
+  return k.hi > k.lo ? (k.hi - 1) / KEYS - k.lo / KEYS + 1 : 1;
+}
+
+// Place in the sequence of units: the item and the keys of one unit.
+template <int ROWS, int KEYS>
+struct Cursor {
+  Request r;
+  Range k;
+  int b, h, tile;
+  int key, unit, units;          // first key of the unit; its place in the item, the item's units
+
+  __device__ __forceinline__ void open(const Params& p) {
+    k = keys_of<ROWS>(p, r, tile);
+    units = units_of<KEYS>(k);
+    unit = 0;
+    key = k.lo / KEYS * KEYS;
+  }
+  __device__ __forceinline__ void next(const Params& p) {
+    key += KEYS;
+    if (++unit < units) return;
+    if (++tile * ROWS >= r.rows) {
+      tile = 0;
+      if (++h == p.c.heads) {
+        h = 0;
+        do {
+          if (++b >= p.t.batch) { units = 0x7fffffff; return; }
+          r = load_request(p, b);
+        } while (!r.rows);
+      }
+    }
+    open(p);
+  }
+};
+
+// Share `blockIdx.x` of gridDim.x: its first unit and the number of its units; every thread of the block calls it.
+template <int ROWS, int KEYS, int THREADS>
+__device__ __forceinline__ long long find_share(const Params& p, Cursor<ROWS, KEYS>& c, long long& first, long long& per,
+                                                long long& total) {
+  __shared__ long long sums[THREADS / 32 + 1];
+  __shared__ int place[8];
+  __shared__ long long place_unit;
+  const int tid = threadIdx.x, each = (p.t.batch + THREADS - 1) / THREADS;
+  const int b0 = min(tid * each, p.t.batch), b1 = min(b0 + each, p.t.batch);
+  auto per_head = [&](const Request& r) {
+    long long s = 0;
+    const int tiles = (r.rows + ROWS - 1) / ROWS;
+    for (int t = 0; t < tiles; ++t) s += units_of<KEYS>(keys_of<ROWS>(p, r, t));
+    return s;
+  };
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += per_head(load_request(p, b)) * p.c.heads;
+  long long scan = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, scan, o);
+    if ((tid & 31) >= o) scan += v;
+  }
+  if ((tid & 31) == 31) sums[tid >> 5] = scan;
+  __syncthreads();
+  long long before = 0;
+  total = 0;
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w < (tid >> 5)) before += sums[w];
+    total += sums[w];
+  }
+  before += scan - mine;
+  per = max((total + gridDim.x - 1) / gridDim.x, (long long)p.least_units);
+  first = per * blockIdx.x;
+  const long long count = min(per, total - first);
+  if (count <= 0) return 0;
+  if (first >= before && first < before + mine) {
+    long long left = first - before;
+    int b = b0;
+    Request r;
+    long long u;
+    for (;; ++b) {
+      r = load_request(p, b);
+      u = per_head(r);
+      if (left < u * p.c.heads) break;
+      left -= u * p.c.heads;
+    }
+    const int h = (int)(left / u);
+    left -= h * u;
+    int tile = 0;
+    for (;; ++tile) {
+      const int n = units_of<KEYS>(keys_of<ROWS>(p, r, tile));
+      if (left < n) break;
+      left -= n;
+    }
+    place[0] = b;
+    place[1] = h;
+    place[2] = tile;
+    place_unit = left;
+  }
+  __syncthreads();
+  c.b = place[0];
+  c.h = place[1];
+  c.tile = place[2];
+  c.r = load_request(p, c.b);
+  c.open(p);
+  c.unit = (int)place_unit;
+  c.key += c.unit * KEYS;
+  return count;
+}
+
+// Output row of tile row `row` of an item: element offset in a [tokens, q_heads, dim] array and the place in lse.
+__device__ __forceinline__ long long token_of(const Params& p, int q0, int row) { return q0 + row / p.group; }
+__device__ __forceinline__ int head_of(const Params& p, int h, int row) { return h * p.group + row % p.group; }
+
+template <typename T> __device__ __forceinline__ uint32_t pack2of(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2of<__nv_bfloat16>(float a, float b) { return tc::pack_bf16(a, b); }
+template <> __device__ __forceinline__ uint32_t pack2of<__half>(float a, float b) {
+  const __half2 t = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+
+// Joins the shares of the items that no share holds alone: one warp per (item, row).  A share leaves at most one item open, its
+// last, which its own slot 1 and slot 0 of the following shares hold.
+template <typename T, int ROWS, int DIM>
+__global__ void __launch_bounds__(128) attend_join_kernel(Params p) {
+  wait_for_previous_kernel();
+  const int share = blockIdx.x;
+  const int4 item = p.open[2 * share], more = p.open[2 * share + 1];
+  const int row = blockIdx.y * 4 + warp_index(), lane = threadIdx.x & 31;
+  if (more.x <= share || row >= item.w) return;
+  constexpr long long kSlot = (long long)ROWS * (DIM + 2);
+  auto slot_of = [&](int s) { return p.part + (2ll * s + (s == share)) * kSlot; };
+  float top = -INFINITY;
+  for (int s = share + lane; s <= more.x; s += 32) top = fmaxf(top, slot_of(s)[ROWS * DIM + row]);
+  top = warp_max(top);
+  const float safe = top == -INFINITY ? 0.f : top;
+  constexpr int kPer = DIM / 32;
+  float o[kPer], sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int s = share; s <= more.x; ++s) {
+    const float* slot = slot_of(s);
+    const float w = exp2f(slot[ROWS * DIM + row] - safe);
+    sum += w * slot[ROWS * (DIM + 1) + row];
+    const float* x = slot + row * DIM + lane * kPer;
+    if constexpr (kPer == 4) {
+      const float4 v = *reinterpret_cast<const float4*>(x);
+      o[0] += w * v.x; o[1] += w * v.y; o[2] += w * v.z; o[3] += w * v.w;
+    } else {
+      const float2 v = *reinterpret_cast<const float2*>(x);
+      o[0] += w * v.x; o[1] += w * v.y;
+    }
+  }
+  const float inv = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
+  const long long token = token_of(p, item.x, item.z + row);
+  const int qh = head_of(p, item.y, item.z + row);
+  T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM + lane * kPer;
+  uint32_t w[kPer / 2];
+#pragma unroll
+  for (int e = 0; e < kPer / 2; ++e) w[e] = pack2of<T>(o[2 * e] * inv, o[2 * e + 1] * inv);
+  if constexpr (kPer == 4) *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint32_t*>(out) = w[0];
+  if (p.lse && lane == 0) p.lse[token * p.q_heads + qh] = 0.69314718055994531f * (safe + log2f(sum));
+}
+
+}  // namespace attend
+}  // namespace covspec

@@ -1,0 +1,384 @@
+// Attention of few rows per key head (single tokens, drafted blocks) over the paged cache: one pass over the keys with running
+// maxima and sums.  A tile is 16, 32 or 64 rows (16 a warp; warps left over share the keys of a unit) and 64 keys.  The work is
+// bound by reading the cache, so operands go to the tensor cores through registers (mma.sync): shared memory holds the pages'
+// rows as they are in the cache, 8-bit ones are widened in registers.
+//
+// 8-bit rows are exact in 16 bits, so their scales stay outside the products: s_ij = (q_i . k_j) * key scale, and the probability
+// takes the value's scale before it is rounded to 16 bits.  So that it cannot leave float16's range, the running maximum is the
+// one of s_ij + log2(value scale).
+#pragma once
+#include "attend_common.cuh"
+
+namespace covspec {
+namespace attend {
+
+constexpr int kKeys = 64;
+constexpr int kThreads = 128;
+
+template <int STORE, int DIM> struct Layout {
+  static constexpr int kBytes = STORE >= cache::kE4M3 ? 1 : 2;
+  static constexpr int kRow = DIM * kBytes;                    // bytes of a key's row
+  static constexpr int kChunks = kRow / 16;
+  static constexpr int kStage = 2 * kKeys * kRow;              // keys, values
+  static constexpr int kStages = kStage >= 32768 ? 3 : kStage >= 16384 ? 5 : 6;
+  static constexpr int kScale = STORE >= cache::kE4M3 ? 3 * kKeys * 4 : 0;   // per stage: key scale, value scale, its log2
+  static constexpr int kJoin = 2 * 16 * (DIM + 4) * 4;         // rows of two warps
+  static constexpr int kSmem = kStages * (kStage + kScale) + kStages * kKeys + kJoin + 128;
+};
+// Byte offset of a 16-byte chunk of a row: chunks are permuted so that eight rows' chunks of one column lie in different banks.
+template <int ROW> __device__ __forceinline__ int swizzled(int row, int chunk) {
+  if constexpr (ROW >= 128) return row * ROW + ((chunk ^ (row & 7)) << 4);
+  else return row * ROW + ((chunk ^ ((row >> 1) & 3)) << 4);
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
+}
+__device__ __forceinline__ void ldm4t(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
+}
+template <typename T>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (sizeof(T) == 2 && __is_same(T, __half))
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Two 8-bit values as two 16-bit ones; `sel` picks their bytes (prmt selector of the low and the high value).  Exact.
+//  e4m3: sign and the seven other bits are moved to where the wider type has them, which is the value over 2^120 (bf16) or 2^8
+//        (f16); the product with that power is exact, subnormal codes included.  The code of NaN does not occur in a cache.
+//  int8: the byte becomes the mantissa of a number with a known exponent, which is then taken off.
+template <typename T, int STORE>
+__device__ __forceinline__ uint32_t widen(uint32_t bytes, uint32_t sel) {
+  uint32_t r;
+  if constexpr (STORE == cache::kE4M3) {
+    const uint32_t w = __byte_perm(bytes, 0u, sel);            // each value in the upper byte of its half, zeros below
+    if constexpr (__is_same(T, __half)) {
+      const uint32_t m = (w & 0x80008000u) | ((w & 0x7f007f00u) >> 1);
+      asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(0x5c005c00u));              // 2^8
+    } else {
+      const uint32_t m = (w & 0x80008000u) | ((w & 0x7f007f00u) >> 4);
+      asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(0x7b807b80u));             // 2^120
+    }
+  } else {
+    if constexpr (__is_same(T, __half)) {
+      const uint32_t w = __byte_perm(bytes ^ 0x80808080u, 0x64646464u, sel);             // 1024 + (v + 128)
+      asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x64806480u));              // - 1152
+    } else {
+      const uint32_t w = __byte_perm(bytes, 0x43434343u, sel);                           // 128 + the lower seven bits ...
+      asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w & 0xff7fff7fu), "r"(w & 0xff80ff80u));   // ... - 128, or 256 for v < 0
+    }
+  }
+  return r;
+}
+// Selectors for the bytes (lo, hi): e4m3 wants them in the upper bytes of the halves, int8 in the lower ones.
+template <int STORE> __device__ constexpr uint32_t pick(int lo, int hi) {
+  return STORE == cache::kE4M3 ? (uint32_t)(4 | lo << 4 | 4 << 8 | hi << 12) : (uint32_t)(lo | 4 << 4 | hi << 8 | 4 << 12);
+}
+
+template <typename T, int STORE, int DIM, int ROWS>
+__global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
+  using L = Layout<STORE, DIM>;
+  constexpr bool k8 = STORE >= cache::kE4M3;
+  constexpr int kWarpsM = ROWS / 16, kWarpsK = 4 / kWarpsM;    // warps along the rows, along the keys of a unit
+  constexpr int kMine = kKeys / kWarpsK;                       // keys of a unit that one warp takes
+  constexpr int kS = L::kStages;
+  extern __shared__ char smem_raw[];
+  char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~(uintptr_t)127);
+  float* scales = reinterpret_cast<float*>(smem + kS * L::kStage);
+  float* join = scales + kS * (L::kScale / 4);
+  unsigned char* there = reinterpret_cast<unsigned char*>(join) + L::kJoin;       // per stage and key: the key is there
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
+  const int wm = warp / kWarpsK, wk = warp % kWarpsK;
+  const int g = lane >> 2, tq = lane & 3;
+
+  wait_for_previous_kernel();
+  Cursor<ROWS, kKeys> load;
+  long long first, per, total;
+  const long long count = find_share<ROWS, kKeys, kThreads>(p, load, first, per, total);
+  const long long share = blockIdx.x;
+  if (count <= 0) {
+    if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
+    launch_dependents_now();
+    return;
+  }
+  Cursor<ROWS, kKeys> at = load;
+
+  // ---- copies of one unit: keys and values of 64 positions, zeros where there is none ----
+  constexpr int kRowsPerPass = kThreads / L::kChunks;
+  const int ld_chunk = tid % L::kChunks, ld_row = tid / L::kChunks;
+  auto copy_unit = [&](int stage) {
+    char* base = smem + stage * L::kStage;
+    const int* table = p.t.table + load.b * p.t.table_ld;
+#pragma unroll
+    for (int pass = 0; pass < kKeys / kRowsPerPass; ++pass) {
+      const int row = pass * kRowsPerPass + ld_row, key = load.key + row;
+      int page = -1;
+      if (key >= load.k.lo && key < load.k.hi) page = table[key >> p.c.page_shift];
+      const bool ok = (unsigned)page < (unsigned)p.c.pages;
+      const long long in = ok ? (((long long)load.h << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1))) : 0;
+      const char* k = static_cast<const char*>(p.c.k) + ((ok ? page * p.c.k_page : 0) + in * DIM) * L::kBytes + ld_chunk * 16;
+      const char* v = static_cast<const char*>(p.c.v) + ((ok ? page * p.c.v_page : 0) + in * DIM) * L::kBytes + ld_chunk * 16;
+      const int off = swizzled<L::kRow>(row, ld_chunk);
+      copy16(tc::smem_u32(base + off), k, ok);
+      copy16(tc::smem_u32(base + kKeys * L::kRow + off), v, ok);
+      if (ld_chunk == 0) {
+        there[stage * kKeys + row] = ok;
+        if constexpr (k8) {
+          float* s = scales + stage * 3 * kKeys + row;
+          const long long w = (((long long)page * p.c.heads) << p.c.page_shift) + in;
+          const float vs = ok ? p.c.v_scale[w] : 1.f;
+          s[0] = (ok ? p.c.k_scale[w] : 0.f) * p.scale_log2;
+          s[kKeys] = vs;
+          s[2 * kKeys] = log2f(fmaxf(vs, cache::kLeastScale));
+        }
+      }
+    }
+  };
+  long long issued = 0;
+  for (int s = 0; s < kS - 1; ++s) {
+    if (issued < count) {
+      copy_unit(s);
+      if (++issued < count) load.next(p);
+    }
+    copies_close();
+  }
+
+  uint32_t qf[DIM / 16][4];
+  float o[DIM / 8][4], top[2], sum[2];
+  int pos[2];                     // position of the thread's two rows; -1 where there is no row
+  long long item_first = first - at.unit;   // the item's first unit
+  bool fresh = true;
+  int stage = 0;
+  for (long long u = 0; u < count; ++u) {
+    if (fresh) {                  // a new item: its query rows
+      fresh = false;
+      item_first = first + u - at.unit;
+      const int r0 = at.tile * ROWS + wm * 16 + g;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = r0 + 8 * i;
+        const bool ok = r < at.r.rows;
+        pos[i] = ok ? at.r.length - at.r.n + r / p.group : -1;
+        const T* q = static_cast<const T*>(p.q) + (ok ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM : 0);
+#pragma unroll
+        for (int s = 0; s < DIM / 16; ++s) {
+          // the order of the products' inner index is free: 8-bit keys come as four neighbours a thread
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(q + 16 * s);
+          qf[s][i] = ok ? w[k8 ? 2 * tq : tq] : 0u;
+          qf[s][2 + i] = ok ? w[k8 ? 2 * tq + 1 : tq + 4] : 0u;
+        }
+        top[i] = -INFINITY;
+        sum[i] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < DIM / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+    }
+    copies_wait<kS - 2>();
+    __syncthreads();
+    {
+      const int into = stage == 0 ? kS - 1 : stage - 1;
+      if (issued < count) {
+        copy_unit(into);
+        if (++issued < count) load.next(p);
+      }
+      copies_close();
+    }
+    // ---- scores of this warp's keys ----
+    const char* kbase = smem + stage * L::kStage;
+    const char* vbase = kbase + kKeys * L::kRow;
+    float s[kMine / 8][4];
+#pragma unroll
+    for (int j = 0; j < kMine / 8; ++j) {
+      s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+      const int row = wk * kMine + j * 8 + (lane & 7);
+#pragma unroll
+      for (int c = 0; c < L::kChunks; c += 4) {
+        uint32_t kf[4];
+        ldm4(kf, tc::smem_u32(kbase + swizzled<L::kRow>(row, c + (lane >> 3))));
+        if constexpr (k8) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            mma<T>(s[j], qf[c + i], widen<T, STORE>(kf[i], pick<STORE>(0, 1)), widen<T, STORE>(kf[i], pick<STORE>(2, 3)));
+        } else {
+          mma<T>(s[j], qf[c / 2], kf[0], kf[1]);
+          mma<T>(s[j], qf[c / 2 + 1], kf[2], kf[3]);
+        }
+      }
+    }
+    // ---- running maxima and sums ----
+    const unsigned char* here = there + stage * kKeys + wk * kMine;
+    const float* sc = scales + stage * 3 * kKeys + wk * kMine;
+    float best[2] = {top[0], top[1]};
+#pragma unroll
+    for (int j = 0; j < kMine / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int col = j * 8 + 2 * tq + (e & 1), key = at.key + wk * kMine + col, i = e >> 1;
+        const bool see = here[col] && key <= pos[i] && (p.window == 0 || key > pos[i] - p.window);
+        s[j][e] = see ? s[j][e] * (k8 ? sc[col] : p.scale_log2) : -INFINITY;
+        best[i] = fmaxf(best[i], k8 ? s[j][e] + sc[2 * kKeys + col] : s[j][e]);
+      }
+    float safe[2], shrink[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 1));
+      best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 2));
+      safe[i] = best[i] == -INFINITY ? 0.f : best[i];
+      shrink[i] = exp2f(top[i] - safe[i]);
+      top[i] = best[i];
+      sum[i] *= shrink[i];
+    }
+#pragma unroll
+    for (int j = 0; j < DIM / 8; ++j) { o[j][0] *= shrink[0]; o[j][1] *= shrink[0]; o[j][2] *= shrink[1]; o[j][3] *= shrink[1]; }
+    uint32_t pf[kMine / 16][4];
+#pragma unroll
+    for (int j = 0; j < kMine / 8; ++j) {
+      float e[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        e[x] = exp2f(s[j][x] - safe[x >> 1]);
+        sum[x >> 1] += e[x];
+        if constexpr (k8) e[x] *= sc[kKeys + j * 8 + 2 * tq + (x & 1)];
+      }
+      pf[j / 2][(j & 1) * 2] = pack2of<T>(e[0], e[1]);
+      pf[j / 2][(j & 1) * 2 + 1] = pack2of<T>(e[2], e[3]);
+    }
+    // ---- values ----
+#pragma unroll
+    for (int s16 = 0; s16 < kMine / 16; ++s16) {
+      const int row0 = wk * kMine + s16 * 16;
+      if constexpr (k8) {
+#pragma unroll
+        for (int c = 0; c < L::kChunks; c += 2) {              // 32 features: chunks c, c + 1 of the 16 keys
+          uint32_t vf[4];                                      // [chunk][keys 0-7, 8-15]
+          ldm4t(vf, tc::smem_u32(vbase + swizzled<L::kRow>(row0 + (lane & 15), c + (lane >> 4))));
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            // a register holds features 2n, 2n + 1 of two keys: the even ones make one tile of eight columns, the odd ones another
+            mma<T>(o[2 * (c + h)], pf[s16], widen<T, STORE>(vf[2 * h], pick<STORE>(0, 2)), widen<T, STORE>(vf[2 * h + 1], pick<STORE>(0, 2)));
+            mma<T>(o[2 * (c + h) + 1], pf[s16], widen<T, STORE>(vf[2 * h], pick<STORE>(1, 3)), widen<T, STORE>(vf[2 * h + 1], pick<STORE>(1, 3)));
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < L::kChunks; c += 2) {
+          uint32_t vf[4];
+          ldm4t(vf, tc::smem_u32(vbase + swizzled<L::kRow>(row0 + (lane & 15), c + (lane >> 4))));
+          mma<T>(o[c], pf[s16], vf[0], vf[1]);
+          mma<T>(o[c + 1], pf[s16], vf[2], vf[3]);
+        }
+      }
+    }
+    stage = stage + 1 == kS ? 0 : stage + 1;
+
+    // ---- the item's end, or the share's ----
+    const bool last = at.unit + 1 == at.units;
+    if (last || u + 1 == count) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+      }
+      // warps that shared the keys: the upper half hands its rows to the lower one, until one has all
+      constexpr int kPitch = DIM + 4;
+#pragma unroll
+      for (int half = kWarpsK / 2; half > 0; half >>= 1) {
+        __syncthreads();
+        float* box = join + (kWarpsK == 4 ? (wk & (half - 1)) : wm) * 16 * kPitch;
+        if (wk >= half && wk < 2 * half) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float* x = box + (g + 8 * i) * kPitch;
+#pragma unroll
+            for (int j = 0; j < DIM / 8; ++j) *reinterpret_cast<float2*>(x + j * 8 + 2 * tq) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
+            if (tq == 0) *reinterpret_cast<float2*>(x + DIM) = make_float2(top[i], sum[i]);
+          }
+        }
+        __syncthreads();
+        if (wk < half) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float* x = box + (g + 8 * i) * kPitch;
+            const float2 ts = *reinterpret_cast<const float2*>(x + DIM);
+            const float both = fmaxf(top[i], ts.x), ref = both == -INFINITY ? 0.f : both;
+            const float a = exp2f(top[i] - ref), b = exp2f(ts.x - ref);
+            top[i] = both;
+            sum[i] = sum[i] * a + ts.y * b;
+#pragma unroll
+            for (int j = 0; j < DIM / 8; ++j) {
+              const float2 v = *reinterpret_cast<const float2*>(x + j * 8 + 2 * tq);
+              o[j][2 * i] = o[j][2 * i] * a + v.x * b;
+              o[j][2 * i + 1] = o[j][2 * i + 1] * a + v.y * b;
+            }
+          }
+        }
+      }
+      const bool whole = last && item_first >= first;
+      if (wk == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int in = wm * 16 + g + 8 * i, r = at.tile * ROWS + in;
+          if (r < at.r.rows) {
+            if (whole) {
+              const float inv = sum[i] > 0.f ? 1.f / sum[i] : (sum[i] == sum[i] ? 0.f : sum[i]);
+              const long long token = token_of(p, at.r.q0, r);
+              const int qh = head_of(p, at.h, r);
+              T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM;
+              if constexpr (k8) {
+#pragma unroll
+                for (int j = 0; j < DIM / 8; j += 2)
+                  *reinterpret_cast<uint2*>(out + j * 8 + 4 * tq) = make_uint2(pack2of<T>(o[j][2 * i] * inv, o[j + 1][2 * i] * inv),
+                                                                              pack2of<T>(o[j][2 * i + 1] * inv, o[j + 1][2 * i + 1] * inv));
+              } else {
+#pragma unroll
+                for (int j = 0; j < DIM / 8; ++j)
+                  *reinterpret_cast<uint32_t*>(out + j * 8 + 2 * tq) = pack2of<T>(o[j][2 * i] * inv, o[j][2 * i + 1] * inv);
+              }
+              if (p.lse && tq == 0)
+                p.lse[token * p.q_heads + qh] = 0.69314718055994531f * ((top[i] == -INFINITY ? 0.f : top[i]) + log2f(sum[i]));
+            } else {
+              float* slot = p.part + (2 * share + (item_first >= first)) * (long long)(ROWS * (DIM + 2));
+              float* x = slot + in * DIM;
+              if constexpr (k8) {
+#pragma unroll
+                for (int j = 0; j < DIM / 8; j += 2)
+                  *reinterpret_cast<float4*>(x + j * 8 + 4 * tq) = make_float4(o[j][2 * i], o[j + 1][2 * i], o[j][2 * i + 1], o[j + 1][2 * i + 1]);
+              } else {
+#pragma unroll
+                for (int j = 0; j < DIM / 8; ++j) *reinterpret_cast<float2*>(x + j * 8 + 2 * tq) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
+              }
+              if (tq == 0) {
+                slot[ROWS * DIM + in] = top[i];
+                slot[ROWS * (DIM + 1) + in] = sum[i];
+              }
+            }
+          }
+        }
+      }
+      if (u + 1 == count && tid == 0) {
+        const bool open = !last && item_first >= first;
+        const long long end = item_first + at.units - 1;       // the item's last unit
+        p.open[2 * share] = make_int4(at.r.q0, at.h, at.tile * ROWS, min(ROWS, at.r.rows - at.tile * ROWS));
+        p.open[2 * share + 1] = make_int4(open ? (int)(end / per) : -1, 0, 0, 0);
+      }
+      fresh = true;
+    }
+    if (u + 1 < count) at.next(p);
+  }
+  launch_dependents_now();
+}
+
+}  // namespace attend
+}  // namespace covspec

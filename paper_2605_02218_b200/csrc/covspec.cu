@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "host.cuh"
 #include "correct_kernels.cuh"
 #include "eig_kernels.cuh"
 #include "gemm_simt.cuh"
@@ -29,17 +30,6 @@
 using namespace covspec;
 
 namespace {
-
-thread_local std::string g_cuda_error;
-
-#define CUDA_TRY(expr)                                                                  \
-  do {                                                                                  \
-    cudaError_t e_ = (expr);                                                            \
-    if (e_ != cudaSuccess) {                                                            \
-      g_cuda_error = std::string(#expr) + ": " + cudaGetErrorString(e_);                \
-      return COVSPEC_ERR_CUDA;                                                          \
-    }                                                                                   \
-  } while (0)
 
 inline long long round_up(long long v, long long a) { return (v + a - 1) / a * a; }
 
@@ -449,36 +439,6 @@ int get_plan(covspec_ctx* ctx, const covspec_problem* p, cudaStream_t stream) {
     ++(ctx)->launches;                                  \
     CUDA_TRY(cudaGetLastError());                       \
   } while (0)
-
-// Launch that may overlap the end of the kernel before it on the stream; the kernel calls
-// wait_for_previous_kernel (common.cuh) before it uses anything of that kernel's.  About 2 us less between two
-// short kernels.  cluster > 1: CTAs per cluster (kernels without a size of their own).
-template <typename... P, typename... A>
-cudaError_t launch_clusters(int cluster, bool dependent, void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s,
-                            A... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2]{};
-  cfg.attrs = attr;
-  if (dependent) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
-  }
-  if (cluster > 1) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-    attr[cfg.numAttrs].val.clusterDim.x = (unsigned)cluster;
-    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
-    ++cfg.numAttrs;
-  }
-  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-}
-template <typename... P, typename... A>
-cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
-  return launch_clusters(1, true, kernel, grid, threads, smem, s, args...);
-}
 
 // Gram matrices of the stage-2 requests: `row` is the map of the row operand.  2 or 4 CTAs per item while that leaves every
 // CTA a single one.

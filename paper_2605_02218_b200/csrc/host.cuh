@@ -1,0 +1,50 @@
+// What the host parts of the library share: the text of the last CUDA error and the launches with attributes.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <string>
+
+namespace covspec {
+
+inline thread_local std::string g_cuda_error;
+
+#define CUDA_TRY(expr)                                                                  \
+  do {                                                                                  \
+    cudaError_t e_ = (expr);                                                            \
+    if (e_ != cudaSuccess) {                                                            \
+      ::covspec::g_cuda_error = std::string(#expr) + ": " + cudaGetErrorString(e_);     \
+      return COVSPEC_ERR_CUDA;                                                          \
+    }                                                                                   \
+  } while (0)
+
+// Launch that may overlap the end of the kernel before it on the stream; the kernel calls
+// wait_for_previous_kernel (common.cuh) before it uses anything of that kernel's.  About 2 us less between two
+// short kernels.  cluster > 1: CTAs per cluster (kernels without a size of their own).
+template <typename... P, typename... A>
+cudaError_t launch_clusters(int cluster, bool dependent, void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s,
+                            A... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2]{};
+  cfg.attrs = attr;
+  if (dependent) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = (unsigned)cluster;
+    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+template <typename... P, typename... A>
+cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
+  return launch_clusters(1, true, kernel, grid, threads, smem, s, args...);
+}
+
+}  // namespace covspec

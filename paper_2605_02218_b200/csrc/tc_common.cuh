@@ -225,7 +225,7 @@ __device__ __forceinline__ void mbar_arrive_release_at(uint32_t cluster_addr) {
 
 // Self-test of the bounded wait: one thread waits on a barrier that nothing signals; the wait gives
 // up after `limit` polls and the time-out is recorded in the status word, exactly as the kernels do.
-__global__ void wait_timeout_selftest_kernel(int* status, uint32_t limit) {
+static __global__ void wait_timeout_selftest_kernel(int* status, uint32_t limit) {
   __shared__ uint64_t bar;
   __shared__ int abort_flag;
   if (threadIdx.x == 0) {

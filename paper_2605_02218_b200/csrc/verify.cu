@@ -1,0 +1,269 @@
+// Host part of the verification operators: argument checks and launches of the paged cache, the attention over it and the edits
+// of logits (include/covspec.h).
+#include "covspec.h"
+
+#include <limits.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "attend_kernels.cuh"
+#include "host.cuh"
+#include "logits_kernels.cuh"
+
+using namespace covspec;
+
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+int bytes_of(int dtype) { return dtype == COVSPEC_F32 ? 4 : dtype == COVSPEC_BF16 || dtype == COVSPEC_F16 ? 2 : 1; }
+bool is_dtype(int dtype) { return dtype == COVSPEC_F32 || dtype == COVSPEC_BF16 || dtype == COVSPEC_F16; }
+
+// Once for each device: the kernel's limit of dynamic shared memory.
+template <auto Kernel>
+cudaError_t allow_shared(int bytes) {
+  static std::atomic<unsigned long long> configured{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1ull)) {
+    e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
+  }
+  return cudaSuccess;
+}
+
+int check_cache(const covspec_cache* c) {
+  if (!c || !c->k || !c->v) return COVSPEC_ERR_ARG;
+  if (c->store < COVSPEC_F32 || c->store > COVSPEC_INT8) return COVSPEC_ERR_ARG;
+  if (c->store >= COVSPEC_E4M3 && (!c->k_scale || !c->v_scale)) return COVSPEC_ERR_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return COVSPEC_ERR_UNSUPPORTED;
+  if (c->page_size < 1 || c->page_size > 4096 || (c->page_size & (c->page_size - 1))) return COVSPEC_ERR_UNSUPPORTED;
+  if (c->pages < 1 || c->heads < 1 || (long long)c->heads * c->page_size * c->head_dim > INT_MAX) return COVSPEC_ERR_SHAPE;
+  const long long least = (long long)c->heads * c->page_size * c->head_dim;
+  if (c->k_page_stride < least || c->v_page_stride < least) return COVSPEC_ERR_SHAPE;
+  const int e = bytes_of(c->store);
+  if (c->k_page_stride * e % 16 || c->v_page_stride * e % 16 || !aligned16(c->k) || !aligned16(c->v)) return COVSPEC_ERR_ARG;
+  return COVSPEC_OK;
+}
+int check_tokens(const covspec_tokens* t) {
+  if (!t || !t->offsets || !t->lengths || !t->table) return COVSPEC_ERR_ARG;
+  if (t->batch < 1 || t->table_width < 1 || t->table_stride < t->table_width) return COVSPEC_ERR_SHAPE;
+  return COVSPEC_OK;
+}
+cache::Pages pages_of(const covspec_cache* c) {
+  cache::Pages p{};
+  p.k = c->k; p.v = c->v; p.k_scale = c->k_scale; p.v_scale = c->v_scale;
+  p.k_page = c->k_page_stride; p.v_page = c->v_page_stride;
+  p.pages = c->pages; p.heads = c->heads;
+  while ((1 << p.page_shift) < c->page_size) ++p.page_shift;
+  return p;
+}
+cache::Tokens tokens_of(const covspec_tokens* t) {
+  return cache::Tokens{t->batch, t->offsets, t->lengths, t->table, t->table_stride, t->table_width};
+}
+
+// Calls f with a null pointer of the type and the constants that the arguments name.
+template <typename F>
+cudaError_t with_type(int dtype, F f) {
+  return dtype == COVSPEC_F32 ? f((float*)nullptr) : dtype == COVSPEC_BF16 ? f((__nv_bfloat16*)nullptr) : f((__half*)nullptr);
+}
+template <int V> using Const = std::integral_constant<int, V>;
+template <typename F>
+cudaError_t with_store(int store, F f) {
+  switch (store) {
+    case COVSPEC_F32: return f(Const<cache::kF32>());
+    case COVSPEC_BF16: return f(Const<cache::kBF16>());
+    case COVSPEC_F16: return f(Const<cache::kF16>());
+    case COVSPEC_E4M3: return f(Const<cache::kE4M3>());
+    default: return f(Const<cache::kInt8>());
+  }
+}
+template <typename F>
+cudaError_t with_dim(int dim, F f) { return dim == 64 ? f(Const<64>()) : f(Const<128>()); }
+
+int sm_count(int* sms) {
+  int dev = 0;
+  CUDA_TRY(cudaGetDevice(&dev));
+  CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  return COVSPEC_OK;
+}
+
+// CTAs of the attention kernel for few rows: two per SM.
+constexpr int kRowsCtas = 2;
+long long part_bytes(int ctas, int rows, int dim) { return 2ll * ctas * rows * (dim + 2) * 4; }
+
+template <typename T, int STORE, int DIM, int ROWS>
+cudaError_t launch_rows(const attend::Params& prm, int ctas, cudaStream_t s) {
+  constexpr auto kernel = attend::attend_kernel<T, STORE, DIM, ROWS>;
+  constexpr int smem = attend::Layout<STORE, DIM>::kSmem;
+  cudaError_t e = allow_shared<kernel>(smem);
+  if (e != cudaSuccess) return e;
+  e = launch_dependent(kernel, dim3((unsigned)ctas), attend::kThreads, smem, s, prm);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(attend::attend_join_kernel<T, ROWS, DIM>, dim3((unsigned)ctas, ROWS / 4), 128, 0, s, prm);
+}
+
+}  // namespace
+
+extern "C" {
+
+int covspec_cache_write(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* k, const void* v,
+                        long long k_stride, long long v_stride, const int* rows, const int* row_offsets, int source_rows,
+                        void* stream) {
+  int st = check_cache(cache);
+  if (st == COVSPEC_OK) st = check_tokens(tokens);
+  if (st != COVSPEC_OK) return st;
+  if (!is_dtype(dtype) || (rows && !row_offsets)) return COVSPEC_ERR_ARG;
+  if (n < 0 || source_rows < 0 || (!rows && source_rows < n)) return COVSPEC_ERR_SHAPE;
+  if (n == 0) return COVSPEC_OK;
+  const long long width = (long long)cache->heads * cache->head_dim;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return COVSPEC_ERR_ARG;
+  if (k_stride < width || v_stride < width) return COVSPEC_ERR_SHAPE;
+  if (k_stride * bytes_of(dtype) % 16 || v_stride * bytes_of(dtype) % 16) return COVSPEC_ERR_ARG;
+  const long long grid = ((long long)n * cache->heads * (cache->head_dim / 8) + cache::kThreads - 1) / cache::kThreads;
+  if (grid > INT_MAX) return COVSPEC_ERR_SHAPE;
+  cache::WriteParams prm{pages_of(cache), tokens_of(tokens), k, v, k_stride, v_stride, n, rows, row_offsets, source_rows};
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  CUDA_TRY(with_type(dtype, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    return with_store(cache->store, [&](auto store) {
+      return with_dim(cache->head_dim, [&](auto dim) {
+        cache::write_kernel<T, decltype(store)::value, decltype(dim)::value><<<(unsigned)grid, cache::kThreads, 0, s>>>(prm);
+        return cudaGetLastError();
+      });
+    });
+  }));
+  return COVSPEC_OK;
+}
+
+int covspec_cache_read(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, void* k, void* v, void* stream) {
+  int st = check_cache(cache);
+  if (st == COVSPEC_OK) st = check_tokens(tokens);
+  if (st != COVSPEC_OK) return st;
+  if (!is_dtype(dtype)) return COVSPEC_ERR_ARG;
+  if (n < 0) return COVSPEC_ERR_SHAPE;
+  if (n == 0) return COVSPEC_OK;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return COVSPEC_ERR_ARG;
+  const long long grid = ((long long)n * cache->heads * (cache->head_dim / 8) + cache::kThreads - 1) / cache::kThreads;
+  if (grid > INT_MAX) return COVSPEC_ERR_SHAPE;
+  cache::ReadParams prm{pages_of(cache), tokens_of(tokens), k, v, n};
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  CUDA_TRY(with_type(dtype, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    return with_store(cache->store, [&](auto store) {
+      return with_dim(cache->head_dim, [&](auto dim) {
+        cache::read_kernel<T, decltype(store)::value, decltype(dim)::value><<<(unsigned)grid, cache::kThreads, 0, s>>>(prm);
+        return cudaGetLastError();
+      });
+    });
+  }));
+  return COVSPEC_OK;
+}
+
+long long covspec_cache_attend_workspace(const covspec_cache* cache, int q_heads) {
+  const int st = check_cache(cache);
+  if (st != COVSPEC_OK) return st;
+  if (q_heads < 1 || q_heads % cache->heads) return COVSPEC_ERR_SHAPE;
+  int sms = 0;
+  if (const int e = sm_count(&sms)) return e;
+  return part_bytes(kRowsCtas * sms, 64, cache->head_dim) + 32ll * kRowsCtas * sms;
+}
+
+int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
+                         long long q_stride, int q_heads, float scale, int window, int max_new, void* out, long long out_stride,
+                         float* lse, void* workspace, long long workspace_bytes, void* stream) {
+  int st = check_cache(cache);
+  if (st == COVSPEC_OK) st = check_tokens(tokens);
+  if (st != COVSPEC_OK) return st;
+  if (dtype != COVSPEC_BF16 && dtype != COVSPEC_F16) return COVSPEC_ERR_UNSUPPORTED;
+  if (cache->store != dtype && cache->store < COVSPEC_E4M3) return COVSPEC_ERR_UNSUPPORTED;
+  if (n < 0 || q_heads < 1 || q_heads % cache->heads || (long long)n * q_heads > INT_MAX / 2) return COVSPEC_ERR_SHAPE;
+  if (window < 0 || max_new < 0 || !(scale == scale)) return COVSPEC_ERR_ARG;
+  if (n == 0) return COVSPEC_OK;
+  const long long width = (long long)q_heads * cache->head_dim;
+  if (!q || !out || !workspace || !aligned16(q) || !aligned16(out) || !aligned16(workspace)) return COVSPEC_ERR_ARG;
+  if (q_stride < width || out_stride < width) return COVSPEC_ERR_SHAPE;
+  if (q_stride % 8 || out_stride % 8) return COVSPEC_ERR_ARG;
+  const long long need = covspec_cache_attend_workspace(cache, q_heads);
+  if (need < 0) return (int)need;
+  if (workspace_bytes < need) return COVSPEC_ERR_WORKSPACE;
+  int sms = 0;
+  if (const int e = sm_count(&sms)) return e;
+
+  attend::Params prm{};
+  prm.c = pages_of(cache);
+  prm.t = tokens_of(tokens);
+  prm.q = q; prm.out = out; prm.lse = lse;
+  prm.q_ld = q_stride; prm.out_ld = out_stride;
+  prm.n = n; prm.q_heads = q_heads; prm.group = q_heads / cache->heads;
+  prm.window = std::min(window, 1 << 30);
+  prm.scale_log2 = scale * 1.4426950408889634f;
+  prm.rows_over = 0; prm.rows_upto = INT_MAX;
+  prm.least_units = 1;
+  prm.open = static_cast<int4*>(workspace);
+  prm.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + 32ll * kRowsCtas * sms);
+  // rows of a key head in the largest request
+  const long long most = (long long)(max_new > 0 ? std::min(max_new, n) : n) * prm.group;
+  const int rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+  // no more CTAs than there can be units
+  const long long items = ((long long)n * prm.group / rows + prm.t.batch) * cache->heads;
+  const long long units = items * (((long long)prm.t.width * cache->page_size + attend::kKeys - 1) / attend::kKeys + 1);
+  const int ctas = (int)std::min<long long>(kRowsCtas * sms, units);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  auto of_type = [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    constexpr int kOwn = std::is_same_v<T, __half> ? cache::kF16 : cache::kBF16;
+    return with_dim(cache->head_dim, [&](auto dim) {
+      constexpr int kDim = decltype(dim)::value;
+      auto of_store = [&](auto store) {
+        constexpr int kStore = decltype(store)::value;
+        return rows == 16 ? launch_rows<T, kStore, kDim, 16>(prm, ctas, s)
+               : rows == 32 ? launch_rows<T, kStore, kDim, 32>(prm, ctas, s) : launch_rows<T, kStore, kDim, 64>(prm, ctas, s);
+      };
+      return cache->store == COVSPEC_E4M3 ? of_store(Const<cache::kE4M3>())
+             : cache->store == COVSPEC_INT8 ? of_store(Const<cache::kInt8>()) : of_store(Const<kOwn>());
+    });
+  };
+  CUDA_TRY(dtype == COVSPEC_BF16 ? of_type((__nv_bfloat16*)nullptr) : of_type((__half*)nullptr));
+  return COVSPEC_OK;
+}
+
+int covspec_edit_logits(int logit_dtype, int rows, int vocab, long long ld, const void* z, void* out, const covspec_edits* edits,
+                        void* stream) {
+  if (!edits || !edits->row_offsets || !is_dtype(logit_dtype)) return COVSPEC_ERR_ARG;
+  const covspec_edits& e = *edits;
+  if ((e.history && !e.history_offsets) || (e.bias_ids && (!e.bias_values || !e.bias_offsets))) return COVSPEC_ERR_ARG;
+  if (rows < 0 || vocab < 1 || ld < vocab || ld * bytes_of(logit_dtype) % 16 || e.batch < 1 || e.history_len < 0 || e.bias_len < 0 ||
+      (e.mask && e.mask_stride < (vocab + 7) / 8))
+    return COVSPEC_ERR_SHAPE;
+  if (rows == 0) return COVSPEC_OK;
+  if (!z || !out || !aligned16(z) || !aligned16(out)) return COVSPEC_ERR_ARG;
+  edit::Params prm{};
+  prm.z = z; prm.out = out; prm.ld = ld; prm.rows = rows; prm.vocab = vocab; prm.batch = e.batch;
+  prm.row_offsets = e.row_offsets;
+  prm.history = e.history; prm.history_offsets = e.history_offsets; prm.history_len = e.history_len;
+  prm.prompt = e.prompt_lengths; prm.drafted = e.drafted;
+  prm.repetition = e.repetition; prm.presence = e.presence; prm.frequency = e.frequency;
+  prm.bias_ids = e.bias_ids; prm.bias = e.bias_values; prm.bias_offsets = e.bias_offsets; prm.bias_len = e.bias_len;
+  prm.mask = static_cast<const unsigned char*>(e.mask); prm.mask_ld = e.mask_stride;
+  int sms = 0;
+  if (const int st = sm_count(&sms)) return st;
+  prm.segment = 4096;
+  prm.group = 1;
+  const unsigned segments = (unsigned)((vocab + prm.segment - 1) / prm.segment);
+  while (prm.group < 16 && (long long)segments * ((rows + 2 * prm.group - 1) / (2 * prm.group)) >= 4ll * sms) prm.group *= 2;
+  const int groups = (rows + prm.group - 1) / prm.group;
+  if (groups > 65535) return COVSPEC_ERR_SHAPE;
+  const size_t smem = (size_t)prm.segment * (e.bias_ids ? 8 : 4);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  CUDA_TRY(with_type(logit_dtype, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    edit::edit_kernel<T><<<dim3(segments, (unsigned)groups), edit::kThreads, smem, s>>>(prm);
+    return cudaGetLastError();
+  }));
+  return COVSPEC_OK;
+}
+
+}  // extern "C"
