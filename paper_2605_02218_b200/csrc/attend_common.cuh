@@ -95,12 +95,13 @@ struct Cursor {
 };
 
 // Share `blockIdx.x` of gridDim.x: its first unit and the number of its units; every thread of the block calls it.
+// `scratch`: THREADS / 32 + 4 words of shared memory.
 template <int ROWS, int KEYS, int THREADS>
 __device__ __forceinline__ long long find_share(const Params& p, Cursor<ROWS, KEYS>& c, long long& first, long long& per,
-                                                long long& total) {
-  __shared__ long long sums[THREADS / 32 + 1];
-  __shared__ int place[8];
-  __shared__ long long place_unit;
+                                                long long* scratch) {
+  long long* sums = scratch;
+  long long& place_unit = scratch[THREADS / 32];
+  int* place = reinterpret_cast<int*>(scratch + THREADS / 32 + 1);
   const int tid = threadIdx.x, each = (p.t.batch + THREADS - 1) / THREADS;
   const int b0 = min(tid * each, p.t.batch), b1 = min(b0 + each, p.t.batch);
   auto per_head = [&](const Request& r) {
@@ -120,7 +121,7 @@ __device__ __forceinline__ long long find_share(const Params& p, Cursor<ROWS, KE
   if ((tid & 31) == 31) sums[tid >> 5] = scan;
   __syncthreads();
   long long before = 0;
-  total = 0;
+  long long total = 0;
   for (int w = 0; w < THREADS / 32; ++w) {
     if (w < (tid >> 5)) before += sums[w];
     total += sums[w];

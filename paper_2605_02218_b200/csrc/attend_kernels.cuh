@@ -105,8 +105,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
 
   wait_for_previous_kernel();
   Cursor<ROWS, kKeys> load;
-  long long first, per, total;
-  const long long count = find_share<ROWS, kKeys, kThreads>(p, load, first, per, total);
+  __shared__ long long scratch[kThreads / 32 + 4];
+  long long first, per;
+  const long long count = find_share<ROWS, kKeys, kThreads>(p, load, first, per, scratch);
   const long long share = blockIdx.x;
   if (count <= 0) {
     if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);

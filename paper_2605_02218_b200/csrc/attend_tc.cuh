@@ -1,0 +1,534 @@
+// Attention of many rows per key head (chunks of prompts, large blocks) over the paged cache on the tensor cores (tcgen05).
+//
+// An item is 256 rows of one key head, two tiles of 128 that take turns: while the softmax of one tile runs, the tensor core
+// multiplies for the other.  A unit is 128 keys.  TMEM holds S (scores, 128 columns) and O (the rows, `DIM` columns) of both
+// tiles; the probabilities overwrite S in 16 bits and are the A operand of the second product from there.  Keys are K-major, values
+// MN-major (keys are the inner dimension of the second product), both as rows of 64 features in 128-byte swizzled tiles.
+//
+// Warps: 0-3 and 4-7 softmax of tile 0 and 1, a row a thread; 8 issues the products; 9-12 bring queries, keys and values into
+// shared memory: 16-bit rows by asynchronous copies, 8-bit ones through registers, where they are widened (attend_kernels.cuh).
+//
+// The running maximum is only a reference that keeps the exponentials in range: a row whose scores stay within 2^8 of it keeps
+// it, so that O is rescaled seldom, and one pass over S makes the probabilities.  A warp with a row beyond that goes over S again.
+#pragma once
+#include "attend_kernels.cuh"
+
+namespace covspec {
+namespace attend {
+namespace wide {
+
+using namespace tc;
+
+constexpr int kRows = 256, kKeys = 128;
+constexpr int kThreads = 13 * 32;
+constexpr int kProducers = 128;
+constexpr float kSlack = 8.f;               // log2 of how far a score may lie above the reference
+
+template <int STORE, int DIM> struct Layout {
+  static constexpr bool k8 = STORE >= cache::kE4M3;
+  static constexpr int kSlot = kKeys * DIM * 2;                // keys or values of a unit, 16-bit
+  static constexpr int kQ = kRows * DIM * 2;
+  static constexpr int kSlots = k8 ? 4 : 5;
+  static constexpr int kTail = 4 * 16                          // which keys of a unit are there, 4 units
+                               + (k8 ? 4 * 2 * kKeys * 4 : 0)  // scales of 4 units
+                               + 2 * kKeys * 8                 // places of a unit's keys, 2 units
+                               + 256;                          // barriers, TMEM base, scratch
+  static constexpr int kUsed = kQ + kSlots * kSlot + kTail;
+  static constexpr int kSmem = kUsed > 120 * 1024 ? kUsed : 120 * 1024;      // one CTA an SM: each takes all of TMEM
+  static_assert(kSmem <= 232448);
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+template <typename T> __device__ __forceinline__ uint32_t idesc(int n, bool b_mn) {
+  const uint32_t type = __is_same(T, __half) ? 0u : 1u;
+  return (1u << 4) | (type << 7) | (type << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+// Values: 64 features of a key are a 128-byte row, eight keys a swizzled block, the next 64 features `kKeys` rows on.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)((kKeys * 128u) >> 4) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "}\n" ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+      "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+      "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Barrier among `n` threads that tells each whether all came with `v`.
+__device__ __forceinline__ bool barrier_and(int id, int n, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.u32 p, %3, 0;\n"
+      "barrier.cta.red.and.aligned.pred q, %1, %2, p;\n"
+      "selp.u32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)v) : "memory");
+  return r != 0;
+}
+
+// Byte offset of a 16-byte chunk of row `row`, 64 features a block of `rows` rows.
+__device__ __forceinline__ int tile_at(int rows, int row, int chunk) {
+  return (chunk >> 3) * rows * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+}
+
+template <typename T, int STORE, int DIM>
+__global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
+  using L = Layout<STORE, DIM>;
+  constexpr bool k8 = L::k8;
+  constexpr int kSlots = L::kSlots;
+  extern __shared__ __align__(1024) uint8_t wide_smem[];
+  uint8_t* smem = wide_smem;
+  uint8_t* ring = smem + L::kQ;
+  uint8_t* tail = ring + kSlots * L::kSlot;
+  uint32_t* there = reinterpret_cast<uint32_t*>(tail);                       // [4][4]
+  float* scales = reinterpret_cast<float*>(tail + 64);                       // [4][2][kKeys]: key scale * scale_log2, value scale
+  int2* places = reinterpret_cast<int2*>(tail + 64 + (k8 ? 4 * 2 * kKeys * 4 : 0));   // [2][kKeys]: page (-1: none), row in it
+  uint64_t* bars = reinterpret_cast<uint64_t*>(places + 2 * kKeys);
+  uint64_t *full = bars, *empty = bars + 5, *q_full = bars + 10, *q_empty = bars + 11, *s_full = bars + 12, *p_ready = bars + 14,
+           *o_full = bars + 16, *drained = bars + 18;                        // 19 barriers
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, kProducers); mbar_init(empty + i, 1); }
+    mbar_init(q_full, kProducers);
+    mbar_init(q_empty, 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(s_full + i, 1); mbar_init(p_ready + i, 4); mbar_init(o_full + i, 1); }
+    mbar_init(drained, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  wait_for_previous_kernel();
+  Cursor<kRows, kKeys> at;
+  long long first, per;
+  const long long count = find_share<kRows, kKeys, kThreads>(p, at, first, per, reinterpret_cast<long long*>(places));
+  const long long share = blockIdx.x;
+  if (count <= 0) {
+    if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
+    launch_dependents_now();
+    return;
+  }
+  if (warp == 8) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  constexpr uint32_t kO = 256;                                 // first column of O; tile x: S at 128 x, O at kO + 128 x
+
+  if (warp >= 9) {
+    // ---------------- producers ----------------
+    const int t = tid - 9 * 32;
+    uint64_t* waiting[3] = {nullptr, nullptr, nullptr};        // barriers of copies that are under way, the oldest last
+    auto close = [&](uint64_t* bar) {                          // the copies so far belong to `bar`
+      copies_close();
+      if (waiting[2]) { copies_wait<3>(); fence_async_proxy(); mbar_arrive(waiting[2]); }
+      waiting[2] = waiting[1];
+      waiting[1] = waiting[0];
+      waiting[0] = bar;
+    };
+    auto flush = [&] {
+      copies_wait<0>();
+      fence_async_proxy();
+#pragma unroll
+      for (int i = 2; i >= 0; --i) {
+        if (waiting[i]) mbar_arrive(waiting[i]);
+        waiting[i] = nullptr;
+      }
+    };
+    // nothing is waited for while copies that the others may need to get on have not been handed over
+    auto acquire = [&](uint64_t* bar, uint32_t parity) {
+      if (mbar_peek(bar, parity)) return true;
+      flush();
+      return mbar_wait(bar, parity, abort_flag);
+    };
+    int slot = 0;
+    uint32_t phase = 1, q_phase = 1;
+    bool ok = true, fresh = true;
+    auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
+    for (long long u = 0; u < count; ++u) {
+      if (fresh) {
+        fresh = false;
+        ok = ok && acquire(q_empty, q_phase);
+        q_phase ^= 1u;
+        constexpr int kChunks = DIM / 8;
+        const int chunk = t % kChunks;
+#pragma unroll 4
+        for (int row = t / kChunks; row < kRows; row += kProducers / kChunks) {
+          const int r = at.tile * kRows + row;
+          const bool there_is = ok && r < at.r.rows;
+          const T* q = static_cast<const T*>(p.q) +
+                       (there_is ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM + chunk * 8 : 0);
+          copy16(smem_u32(smem + (row >> 7) * (128 * DIM * 2) + tile_at(128, row & 127, chunk)), q, there_is);
+        }
+        close(q_full);
+      }
+      // places of the unit's keys, a key a thread
+      int2* place = places + (u & 1) * kKeys;
+      {
+        const int key = at.key + t;
+        int page = -1;
+        if (key >= at.k.lo && key < at.k.hi) page = p.t.table[at.b * p.t.table_ld + (key >> p.c.page_shift)];
+        const bool is = (unsigned)page < (unsigned)p.c.pages;
+        const int row = (at.h << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1));
+        // the words of unit u - 4 have been read: its products are done (the slot that this unit's keys take says so)
+        ok = ok && acquire(empty + slot, phase);
+        place[t] = make_int2(is ? page : -1, row);
+        const uint32_t word = __ballot_sync(0xffffffffu, is);
+        if (lane == 0) there[(u & 3) * 4 + (t >> 5)] = word;
+        if constexpr (k8) {
+          float* sc = scales + (u & 3) * 2 * kKeys;
+          const long long w = (((long long)page * p.c.heads) << p.c.page_shift) + row;
+          const float vs = is ? p.c.v_scale[w] : 1.f;
+          sc[t] = is ? p.c.k_scale[w] * p.scale_log2 : 0.f;
+          sc[kKeys + t] = vs < cache::kLeastScale ? cache::kLeastScale : vs;
+        }
+      }
+      // all of them go on or none: a thread that has left would be waited for at the next barrier
+      if (!(ok = barrier_and(1, kProducers, ok))) break;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        if (kv && !(ok = acquire(empty + slot, phase))) break;
+        uint8_t* dst = ring + slot * L::kSlot;
+        const char* base = static_cast<const char*>(kv ? p.c.v : p.c.k);
+        const long long page_ld = kv ? p.c.v_page : p.c.k_page;
+        if constexpr (!k8) {
+          constexpr int kChunks = DIM / 8, kStep = kProducers / kChunks;
+          const int chunk = t % kChunks;
+#pragma unroll 4
+          for (int row = t / kChunks; row < kKeys; row += kStep) {
+            const int2 pl = place[row];
+            const bool is = pl.x >= 0;
+            const char* src = base + (is ? (pl.x * page_ld + (long long)pl.y * DIM) * 2 + chunk * 16 : 0);
+            copy16(smem_u32(dst + tile_at(kKeys, row, chunk)), src, is);
+          }
+          close(full + slot);
+        } else {
+          constexpr int kChunks = DIM / 16, kStep = kProducers / kChunks, kPer = kKeys / kStep;
+          const int chunk = t % kChunks;
+          uint4 raw[kPer];
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const int2 pl = place[t / kChunks + i * kStep];
+            raw[i] = pl.x >= 0 ? *reinterpret_cast<const uint4*>(base + pl.x * page_ld + (long long)pl.y * DIM + chunk * 16) : make_uint4(0u, 0u, 0u, 0u);
+          }
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const int row = t / kChunks + i * kStep;
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            uint32_t v[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[2 * e] = widen<T, STORE>(w[e], pick<STORE>(0, 1));
+              v[2 * e + 1] = widen<T, STORE>(w[e], pick<STORE>(2, 3));
+            }
+            *reinterpret_cast<uint4*>(dst + tile_at(kKeys, row, 2 * chunk)) = make_uint4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<uint4*>(dst + tile_at(kKeys, row, 2 * chunk + 1)) = make_uint4(v[4], v[5], v[6], v[7]);
+          }
+          flush();                                             // the queries' copies, if they are still under way
+          mbar_arrive(full + slot);
+        }
+        next_slot();
+      }
+      if (u + 1 < count) {
+        fresh = at.unit + 1 == at.units;
+        at.next(p);
+      }
+    }
+    flush();
+  } else if (warp == 8) {
+    // ---------------- products ----------------
+    const uint32_t qk = idesc<T>(kKeys, false), pv = idesc<T>(DIM, true);
+    int k_slot = 0, slot = 0;                                  // slot of the keys in S, next slot of the ring
+    uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0};
+    bool ok = true;
+    auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
+    auto scores = [&](int x, int s) {
+      const uint32_t a0 = smem_u32(smem + x * (128 * DIM * 2)), b0 = smem_u32(ring + s * L::kSlot);
+#pragma unroll
+      for (int h = 0; h < DIM / 64; ++h) {
+        const uint64_t a = umma_desc(a0 + h * 128 * 128), b = umma_desc(b0 + h * kKeys * 128);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) umma_bf16(tmem + x * 128, a + 2 * k, b + 2 * k, qk, (h | k) != 0);
+      }
+      umma_commit(s_full + x);
+    };
+    auto rows = [&](int x, int s, bool accumulate) {
+      const uint64_t b = desc_mn(smem_u32(ring + s * L::kSlot));
+#pragma unroll
+      for (int k = 0; k < kKeys / 16; ++k)
+        mma_ts(tmem + kO + x * 128, tmem + x * 128 + 8 * k, b + k * (16 * 128 / 16), pv, accumulate || k != 0);
+    };
+    bool fresh = true, opened = false;                         // the next unit begins an item; its scores are issued
+    for (long long u = 0; u < count && ok; ++u) {
+      const bool two = at.r.rows - at.tile * kRows > 128;
+      const bool begins = fresh;
+      if (!opened) {
+        if (fresh) {
+          ok = mbar_wait(q_full, q_phase, abort_flag);
+          q_phase ^= 1u;
+        }
+        ok = ok && mbar_wait(full + slot, phase, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        if (lane == 0) {
+          scores(0, slot);
+          if (two) scores(1, slot);
+          umma_commit(empty + slot);
+        }
+        k_slot = slot;
+        next_slot();
+      }
+      (void)k_slot;
+      opened = false;
+      const bool ends = at.unit + 1 == at.units, more = u + 1 < count && !ends;
+      if (!more && lane == 0) umma_commit(q_empty);
+      const int v_slot = slot;
+      ok = mbar_wait(full + v_slot, phase, abort_flag);
+      if (!ok) break;
+      next_slot();
+      for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
+        ok = mbar_wait(p_ready + x, p_phase[x], abort_flag);
+        p_phase[x] ^= 1u;
+        if (!ok) break;
+        tc_fence_after();
+        if (lane == 0) {
+          rows(x, v_slot, !begins);
+          if (!more) umma_commit(o_full + x);
+          if (x == (two ? 1 : 0)) umma_commit(empty + v_slot);
+        }
+        if (more) {
+          if (x == 0) {
+            ok = mbar_wait(full + slot, phase, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+          }
+          if (lane == 0) scores(x, slot);
+        }
+        __syncwarp();
+      }
+      if (more && ok) {
+        if (lane == 0) umma_commit(empty + slot);
+        k_slot = slot;
+        next_slot();
+        opened = true;
+      }
+      fresh = ends;
+      if (u + 1 < count) at.next(p);
+      __syncwarp();
+    }
+    // TMEM and the ring are free when every product has ended, also after a wait that gave up
+    if (lane == 0) umma_commit(drained);
+    volatile int gave_up = 0;
+    mbar_wait(drained, 0, &gave_up);
+    __syncwarp();
+  } else {
+    // ---------------- softmax ----------------
+    const int x = warp >> 2, row = tid & 127;
+    const uint32_t s_at = tmem + x * 128 + ((uint32_t)(warp & 3) << 21), o_at = s_at + kO;
+    float ref = 0.f, sum = 0.f;
+    int pos = -1;
+    long long item_first = 0;
+    bool fresh = true, ok = true, active = false;
+    uint32_t s_phase = 0, o_phase = 0;
+    for (long long u = 0; u < count; ++u) {
+      const int r = at.tile * kRows + x * 128 + row;
+      if (fresh) {
+        fresh = false;
+        item_first = first + u - at.unit;
+        active = at.r.rows - at.tile * kRows > x * 128;
+        const bool is = r < at.r.rows;
+        pos = is ? at.r.length - at.r.n + r / p.group : -1;
+        ref = is ? -INFINITY : 0.f;                            // rows past the end never ask for a reference
+        sum = 0.f;
+      }
+      if (active) {
+        ok = ok && mbar_wait(s_full + x, s_phase, abort_flag);
+        s_phase ^= 1u;
+        tc_fence_after();
+        const uint4 bits = *reinterpret_cast<const uint4*>(there + (u & 3) * 4);
+        const float* sc = scales + (u & 3) * 2 * kKeys;
+        // every row of the warp sees all keys of the unit
+        const bool clear = (bits.x & bits.y & bits.z & bits.w) == 0xffffffffu &&
+                           __all_sync(0xffffffffu, pos < 0 ? r >= at.r.rows : at.key + kKeys - 1 <= pos && (p.window == 0 || at.key > pos - p.window));
+        const int lowest = p.window ? max(pos - p.window + 1, 0) : 0;
+        // scores of 32 keys: scaled, those not seen -inf
+        auto fetch = [&](int c, float (&v)[32]) {
+          tmem_ld32(s_at + 32 * c, v);
+          if constexpr (k8) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 a = *reinterpret_cast<const float4*>(sc + 32 * c + e);
+              v[e] *= a.x; v[e + 1] *= a.y; v[e + 2] *= a.z; v[e + 3] *= a.w;
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] *= p.scale_log2;
+          }
+          if (!clear) {
+            const uint32_t word = c == 0 ? bits.x : c == 1 ? bits.y : c == 2 ? bits.z : bits.w;
+            const int k0 = at.key + 32 * c;
+            // bits of the keys lowest .. pos
+            uint32_t see = word;
+            see &= pos < k0 ? 0u : pos - k0 >= 31 ? 0xffffffffu : (2u << (pos - k0)) - 1u;
+            see &= lowest <= k0 ? 0xffffffffu : lowest - k0 > 31 ? 0u : ~((1u << (lowest - k0)) - 1u);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : -INFINITY;
+          }
+        };
+        uint32_t packed[64];
+        float top = 0.f, more = 0.f;
+        auto make = [&](float safe) {
+          top = -INFINITY;
+          more = 0.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float v[32];
+            fetch(c, v);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                v[e + i] = ex2(v[e + i] - safe);
+                more += v[e + i];
+              }
+              if constexpr (k8) {
+                const float4 w = *reinterpret_cast<const float4*>(sc + kKeys + 32 * c + e);
+                v[e] *= w.x; v[e + 1] *= w.y; v[e + 2] *= w.z; v[e + 3] *= w.w;
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) top = fmaxf(top, v[e + i]);
+              packed[16 * c + e / 2] = pack2of<T>(v[e], v[e + 1]);
+              packed[16 * c + e / 2 + 1] = pack2of<T>(v[e + 2], v[e + 3]);
+            }
+          }
+        };
+        const bool unset = ref == -INFINITY;
+        bool again = __any_sync(0xffffffffu, unset);
+        if (!again) {
+          make(ref);
+          again = __any_sync(0xffffffffu, top > 256.f);
+        }
+        if (again) {                                           // new references, from the scores themselves
+          float best = ref;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            float v[32];
+            fetch(c, v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) best = fmaxf(best, k8 ? v[e] + log2f(sc[kKeys + 32 * c + e]) : v[e]);
+          }
+          const float old = ref;
+          if (best > ref) ref = best;
+          const float shrink = old == -INFINITY ? 0.f : ex2(old - ref);
+          sum *= shrink;
+          if (first + u > max(item_first, first)) {            // O holds earlier units' rows
+#pragma unroll 1
+            for (int c = 0; c < DIM / 32; ++c) {
+              float v[32];
+              tmem_ld32(o_at + 32 * c, v);
+              uint32_t w[32];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(v[e] * shrink);
+              tmem_st32(o_at + 32 * c, w);
+            }
+            tmem_st_wait();
+          }
+          make(ref == -INFINITY ? 0.f : ref);
+        }
+        sum += more;
+        tmem_st32(s_at, packed);
+        tmem_st32(s_at + 32, packed + 32);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_ready + x);
+      }
+      const bool last = at.unit + 1 == at.units;
+      if (last || u + 1 == count) {
+        const bool whole = last && item_first >= first;
+        if (active) {
+          ok = ok && mbar_wait(o_full + x, o_phase, abort_flag);
+          o_phase ^= 1u;
+          tc_fence_after();
+          const bool is = r < at.r.rows;
+          // a wait that gave up leaves NaN
+          const float inv = !ok ? __int_as_float(0x7fffffff) : sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
+          const long long token = is ? token_of(p, at.r.q0, r) : 0;
+          const int qh = is ? head_of(p, at.h, r) : 0;
+          T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM;
+          float* slot = p.part + (2 * share + (item_first >= first)) * (long long)(kRows * (DIM + 2));
+          const int in = x * 128 + row;
+#pragma unroll 1
+          for (int c = 0; c < DIM / 32; ++c) {
+            float v[32];
+            tmem_ld32(o_at + 32 * c, v);
+            if (is && whole) {
+#pragma unroll
+              for (int e = 0; e < 32; e += 8)
+                *reinterpret_cast<uint4*>(out + 32 * c + e) = make_uint4(pack2of<T>(v[e] * inv, v[e + 1] * inv), pack2of<T>(v[e + 2] * inv, v[e + 3] * inv),
+                                                                         pack2of<T>(v[e + 4] * inv, v[e + 5] * inv), pack2of<T>(v[e + 6] * inv, v[e + 7] * inv));
+            } else if (is) {
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(slot + in * DIM + 32 * c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+            }
+            __syncwarp();
+          }
+          if (is) {
+            if (!whole) {
+              slot[kRows * DIM + in] = ref;
+              slot[kRows * (DIM + 1) + in] = ok ? sum : inv;
+            } else if (p.lse) {
+              p.lse[token * p.q_heads + qh] = ok ? 0.69314718055994531f * ((ref == -INFINITY ? 0.f : ref) + log2f(sum)) : inv;
+            }
+          }
+          tc_fence_before();
+        }
+        if (u + 1 == count && tid == 0) {
+          const bool open = !last && item_first >= first;
+          const long long end = item_first + at.units - 1;
+          p.open[2 * share] = make_int4(at.r.q0, at.h, at.tile * kRows, min(kRows, at.r.rows - at.tile * kRows));
+          p.open[2 * share + 1] = make_int4(open ? (int)(end / per) : -1, 0, 0, 0);
+        }
+        fresh = true;
+      }
+      if (u + 1 < count) at.next(p);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tmem_dealloc(tmem, 512);
+  launch_dependents_now();
+}
+
+}  // namespace wide
+}  // namespace attend
+}  // namespace covspec

@@ -8,6 +8,7 @@
 #include <atomic>
 
 #include "attend_kernels.cuh"
+#include "attend_tc.cuh"
 #include "host.cuh"
 #include "logits_kernels.cuh"
 
@@ -90,8 +91,8 @@ int sm_count(int* sms) {
   return COVSPEC_OK;
 }
 
-// CTAs of the attention kernel for few rows: two per SM.
-constexpr int kRowsCtas = 2;
+// Largest request, as rows of a key head, that the attention kernel for few rows takes when both run; its CTAs: two per SM.
+constexpr int kFewRows = 64, kRowsCtas = 2;
 long long part_bytes(int ctas, int rows, int dim) { return 2ll * ctas * rows * (dim + 2) * 4; }
 
 template <typename T, int STORE, int DIM, int ROWS>
@@ -103,6 +104,17 @@ cudaError_t launch_rows(const attend::Params& prm, int ctas, cudaStream_t s) {
   e = launch_dependent(kernel, dim3((unsigned)ctas), attend::kThreads, smem, s, prm);
   if (e != cudaSuccess) return e;
   return launch_dependent(attend::attend_join_kernel<T, ROWS, DIM>, dim3((unsigned)ctas, ROWS / 4), 128, 0, s, prm);
+}
+
+template <typename T, int STORE, int DIM>
+cudaError_t launch_wide(const attend::Params& prm, int ctas, cudaStream_t s) {
+  constexpr auto kernel = attend::wide::attend_wide_kernel<T, STORE, DIM>;
+  constexpr int smem = attend::wide::Layout<STORE, DIM>::kSmem, rows = attend::wide::kRows;
+  cudaError_t e = allow_shared<kernel>(smem);
+  if (e != cudaSuccess) return e;
+  e = launch_dependent(kernel, dim3((unsigned)ctas), attend::wide::kThreads, smem, s, prm);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(attend::attend_join_kernel<T, rows, DIM>, dim3((unsigned)ctas, rows / 4), 128, 0, s, prm);
 }
 
 }  // namespace
@@ -168,7 +180,8 @@ long long covspec_cache_attend_workspace(const covspec_cache* cache, int q_heads
   if (q_heads < 1 || q_heads % cache->heads) return COVSPEC_ERR_SHAPE;
   int sms = 0;
   if (const int e = sm_count(&sms)) return e;
-  return part_bytes(kRowsCtas * sms, 64, cache->head_dim) + 32ll * kRowsCtas * sms;
+  return part_bytes(kRowsCtas * sms, kFewRows, cache->head_dim) + part_bytes(sms, attend::wide::kRows, cache->head_dim) +
+         32ll * (kRowsCtas + 1) * sms;
 }
 
 int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
@@ -203,14 +216,23 @@ int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* token
   prm.rows_over = 0; prm.rows_upto = INT_MAX;
   prm.least_units = 1;
   prm.open = static_cast<int4*>(workspace);
-  prm.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + 32ll * kRowsCtas * sms);
-  // rows of a key head in the largest request
+  prm.part = reinterpret_cast<float*>(prm.open + 2ll * (kRowsCtas + 1) * sms);
+  // rows of a key head in the largest request.  Where some may have many, each of the two kernels takes its requests
   const long long most = (long long)(max_new > 0 ? std::min(max_new, n) : n) * prm.group;
   const int rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+  const bool both = most > kFewRows;
   // no more CTAs than there can be units
-  const long long items = ((long long)n * prm.group / rows + prm.t.batch) * cache->heads;
-  const long long units = items * (((long long)prm.t.width * cache->page_size + attend::kKeys - 1) / attend::kKeys + 1);
-  const int ctas = (int)std::min<long long>(kRowsCtas * sms, units);
+  auto ctas_of = [&](int rows, int keys, int ctas) {
+    const long long items = ((long long)n * prm.group / rows + prm.t.batch) * cache->heads;
+    return (int)std::min<long long>(ctas, items * (((long long)prm.t.width * cache->page_size + keys - 1) / keys + 1));
+  };
+  const int ctas = ctas_of(rows, attend::kKeys, kRowsCtas * sms);
+  attend::Params wide = prm;
+  wide.rows_over = kFewRows;
+  wide.open = prm.open + 2ll * kRowsCtas * sms;
+  wide.part = prm.part + part_bytes(kRowsCtas * sms, kFewRows, cache->head_dim) / 4;
+  const int wide_ctas = ctas_of(attend::wide::kRows, attend::wide::kKeys, sms);
+  if (both) prm.rows_upto = kFewRows;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   auto of_type = [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
@@ -219,6 +241,8 @@ int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* token
       constexpr int kDim = decltype(dim)::value;
       auto of_store = [&](auto store) {
         constexpr int kStore = decltype(store)::value;
+        if (both)
+          if (const cudaError_t e = launch_wide<T, kStore, kDim>(wide, wide_ctas, s); e != cudaSuccess) return e;
         return rows == 16 ? launch_rows<T, kStore, kDim, 16>(prm, ctas, s)
                : rows == 32 ? launch_rows<T, kStore, kDim, 32>(prm, ctas, s) : launch_rows<T, kStore, kDim, 64>(prm, ctas, s);
       };
