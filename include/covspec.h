@@ -226,7 +226,7 @@ int covspec_correct(int logit_dtype, int rows, int vocab, long long ld, const vo
 
 /* A paged cache of one layer.  A page holds page_size positions of all key heads: [heads, page_size, head_dim], dense, pages
  * k_page_stride (v_page_stride) elements apart, so keys and values may be halves of one array.  Bases and strides are multiples
- * of 16 bytes.
+ * of 16 bytes.  Keys and values take at most 64 GiB each.
  * store: COVSPEC_F32, COVSPEC_BF16, COVSPEC_F16: rows as they are; COVSPEC_E4M3, COVSPEC_INT8: one byte a value and a float32
  * scale for each position and head, [pages, heads, page_size] dense.  A row x is held as x / scale, rounded once, half to even,
  * from the exact quotient, with scale = max(max|x| / L, 2^-100) in float32 and L = 448 or 127.  A row with a value that is not

@@ -97,8 +97,7 @@ struct Cursor {
 // Share `blockIdx.x` of gridDim.x: its first unit and the number of its units; every thread of the block calls it.
 // `scratch`: THREADS / 32 + 4 words of shared memory.
 template <int ROWS, int KEYS, int THREADS>
-__device__ __forceinline__ long long find_share(const Params& p, Cursor<ROWS, KEYS>& c, long long& first, long long& per,
-                                                long long* scratch) {
+__device__ __forceinline__ int find_share(const Params& p, Cursor<ROWS, KEYS>& c, long long& first, long long& per, long long* scratch) {
   long long* sums = scratch;
   long long& place_unit = scratch[THREADS / 32];
   int* place = reinterpret_cast<int*>(scratch + THREADS / 32 + 1);
@@ -129,7 +128,7 @@ __device__ __forceinline__ long long find_share(const Params& p, Cursor<ROWS, KE
   before += scan - mine;
   per = max((total + gridDim.x - 1) / gridDim.x, (long long)p.least_units);
   first = per * blockIdx.x;
-  const long long count = min(per, total - first);
+  const long long count = min(per, total - first);      // a share is far below 2^31 units: one is 64 keys at least
   if (count <= 0) return 0;
   if (first >= before && first < before + mine) {
     long long left = first - before;
@@ -163,7 +162,7 @@ __device__ __forceinline__ long long find_share(const Params& p, Cursor<ROWS, KE
   c.open(p);
   c.unit = (int)place_unit;
   c.key += c.unit * KEYS;
-  return count;
+  return (int)count;
 }
 
 // Output row of tile row `row` of an item: element offset in a [tokens, q_heads, dim] array and the place in lse.

@@ -20,10 +20,10 @@ template <int STORE, int DIM> struct Layout {
   static constexpr int kRow = DIM * kBytes;                    // bytes of a key's row
   static constexpr int kChunks = kRow / 16;
   static constexpr int kStage = 2 * kKeys * kRow;              // keys, values
-  static constexpr int kStages = kStage >= 32768 ? 3 : kStage >= 16384 ? 5 : 6;
-  static constexpr int kScale = STORE >= cache::kE4M3 ? 3 * kKeys * 4 : 0;   // per stage: key scale, value scale, its log2
-  static constexpr int kJoin = 2 * 16 * (DIM + 4) * 4;         // rows of two warps
-  static constexpr int kSmem = kStages * (kStage + kScale) + kStages * kKeys + kJoin + 128;
+  static constexpr int kStages = kStage >= 32768 ? 3 : 6;
+  static constexpr int kScale = STORE >= cache::kE4M3 ? 2 * kKeys * 4 : 0;   // per stage: the keys' and the values' scales
+  static constexpr int kSmem = kStages * (kStage + kScale) + 2 * 2 * kKeys * 4   // places of two units
+                               + (kStages + 1) * 8 + 2 * 16 * 8 + 128;           // keys there; maxima and sums of two warps' rows
 };
 // Byte offset of a 16-byte chunk of a row: chunks are permuted so that eight rows' chunks of one column lie in different banks.
 template <int ROW> __device__ __forceinline__ int swizzled(int row, int chunk) {
@@ -34,7 +34,20 @@ template <int ROW> __device__ __forceinline__ int swizzled(int row, int chunk) {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
 __device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+constexpr uint32_t kNowhere = 0xffffffffu;
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// The exponent of a positive number: near enough to its logarithm for a reference.
+__device__ __forceinline__ float exponent_of(float x) {
+  return __uint_as_float(0x4b000000u | (__float_as_uint(x) >> 23)) - (8388608.f + 127.f);
+}
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
@@ -97,8 +110,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
   extern __shared__ char smem_raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~(uintptr_t)127);
   float* scales = reinterpret_cast<float*>(smem + kS * L::kStage);
-  float* join = scales + kS * (L::kScale / 4);
-  unsigned char* there = reinterpret_cast<unsigned char*>(join) + L::kJoin;       // per stage and key: the key is there
+  uint32_t* places = reinterpret_cast<uint32_t*>(scales + kS * (L::kScale / 4));   // [2][2][kKeys]: keys', values' rows in 16 bytes
+  float2* box_ts = reinterpret_cast<float2*>(places + 4 * kKeys);                  // [2][16]
+  uint32_t* there = reinterpret_cast<uint32_t*>(box_ts + 2 * 16);                  // [kS + 1][2]: which keys of a unit are there
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   const int wm = warp / kWarpsK, wk = warp % kWarpsK;
   const int g = lane >> 2, tq = lane & 3;
@@ -107,8 +121,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
   Cursor<ROWS, kKeys> load;
   __shared__ long long scratch[kThreads / 32 + 4];
   long long first, per;
-  const long long count = find_share<ROWS, kKeys, kThreads>(p, load, first, per, scratch);
-  const long long share = blockIdx.x;
+  const int count = find_share<ROWS, kKeys, kThreads>(p, load, first, per, scratch);
+  const int share = blockIdx.x;
   if (count <= 0) {
     if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
     launch_dependents_now();
@@ -116,62 +130,92 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
   }
   Cursor<ROWS, kKeys> at = load;
 
-  // ---- copies of one unit: keys and values of 64 positions, zeros where there is none ----
+  // ---- copies of one unit: keys and values of 64 positions, zeros where there is none.  The places of its keys, one a thread, are
+  // worked out an iteration before, and the pages are fetched one before that ----
   constexpr int kRowsPerPass = kThreads / L::kChunks;
   const int ld_chunk = tid % L::kChunks, ld_row = tid / L::kChunks;
-  auto copy_unit = [&](int stage) {
-    char* base = smem + stage * L::kStage;
-    const int* table = p.t.table + load.b * p.t.table_ld;
-#pragma unroll
-    for (int pass = 0; pass < kKeys / kRowsPerPass; ++pass) {
-      const int row = pass * kRowsPerPass + ld_row, key = load.key + row;
-      int page = -1;
-      if (key >= load.k.lo && key < load.k.hi) page = table[key >> p.c.page_shift];
+  int page = -1, issued = 0, word = 0;          // page of key `tid` of the unit at `load`; units copied; unit modulo kS + 1
+  [[maybe_unused]] long long scale_at = -1;
+  auto look_up = [&] {
+    const int key = load.key + tid;
+    if (tid < kKeys) page = key >= load.k.lo && key < load.k.hi ? p.t.table[load.b * p.t.table_ld + (key >> p.c.page_shift)] : -1;
+  };
+  auto publish = [&] {
+    if (tid < kKeys && issued < count) {
       const bool ok = (unsigned)page < (unsigned)p.c.pages;
-      const long long in = ok ? (((long long)load.h << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1))) : 0;
-      const char* k = static_cast<const char*>(p.c.k) + ((ok ? page * p.c.k_page : 0) + in * DIM) * L::kBytes + ld_chunk * 16;
-      const char* v = static_cast<const char*>(p.c.v) + ((ok ? page * p.c.v_page : 0) + in * DIM) * L::kBytes + ld_chunk * 16;
-      const int off = swizzled<L::kRow>(row, ld_chunk);
-      copy16(tc::smem_u32(base + off), k, ok);
-      copy16(tc::smem_u32(base + kKeys * L::kRow + off), v, ok);
-      if (ld_chunk == 0) {
-        there[stage * kKeys + row] = ok;
-        if constexpr (k8) {
-          float* s = scales + stage * 3 * kKeys + row;
-          const long long w = (((long long)page * p.c.heads) << p.c.page_shift) + in;
-          const float vs = ok ? p.c.v_scale[w] : 1.f;
-          s[0] = (ok ? p.c.k_scale[w] : 0.f) * p.scale_log2;
-          s[kKeys] = vs;
-          s[2 * kKeys] = log2f(fmaxf(vs, cache::kLeastScale));
+      const int in = (load.h << p.c.page_shift) + ((load.key + tid) & ((1 << p.c.page_shift) - 1));
+      uint32_t* place = places + (issued & 1) * 2 * kKeys + tid;
+      auto row = [&](long long page_ld) { return (uint32_t)((unsigned long long)(page * page_ld + (long long)in * DIM) / (16 / L::kBytes)); };
+      place[0] = ok ? row(p.c.k_page) : kNowhere;
+      place[kKeys] = ok ? row(p.c.v_page) : kNowhere;
+      const uint32_t bits = __ballot_sync(0xffffffffu, ok);
+      if (lane == 0) there[2 * word + warp] = bits;
+      if constexpr (k8) scale_at = ok ? (((long long)page * p.c.heads) << p.c.page_shift) + in : -1;
+    }
+    word = word == kS ? 0 : word + 1;
+  };
+  auto copy_unit = [&](int stage) {
+    if (issued < count) {
+      char* base = smem + stage * L::kStage;
+      const uint32_t* place = places + (issued & 1) * 2 * kKeys;
+      constexpr int kPer = kKeys / kRowsPerPass;
+      uint32_t at[kPer][2];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        at[i][0] = place[i * kRowsPerPass + ld_row];
+        at[i][1] = place[kKeys + i * kRowsPerPass + ld_row];
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int off = swizzled<L::kRow>(i * kRowsPerPass + ld_row, ld_chunk);
+        const bool ok = at[i][0] != kNowhere;
+        copy16(tc::smem_u32(base + off), static_cast<const char*>(p.c.k) + (ok ? (unsigned long long)at[i][0] * 16 + ld_chunk * 16 : 0ull), ok);
+        copy16(tc::smem_u32(base + kKeys * L::kRow + off), static_cast<const char*>(p.c.v) + (ok ? (unsigned long long)at[i][1] * 16 + ld_chunk * 16 : 0ull), ok);
+      }
+      if constexpr (k8) {
+        if (tid < kKeys) {
+          float* s = scales + stage * 2 * kKeys + tid;
+          copy4(tc::smem_u32(s), p.c.k_scale + (scale_at >= 0 ? scale_at : 0), scale_at >= 0);
+          copy4(tc::smem_u32(s + kKeys), p.c.v_scale + (scale_at >= 0 ? scale_at : 0), scale_at >= 0);
         }
       }
-    }
-  };
-  long long issued = 0;
-  for (int s = 0; s < kS - 1; ++s) {
-    if (issued < count) {
-      copy_unit(s);
-      if (++issued < count) load.next(p);
+      if (++issued < count) {
+        load.next(p);
+        look_up();
+      }
     }
     copies_close();
+  };
+  look_up();
+  for (int s = 0; s < kS - 1; ++s) {
+    publish();
+    __syncthreads();
+    copy_unit(s);
   }
 
   uint32_t qf[DIM / 16][4];
   float o[DIM / 8][4], top[2], sum[2];
   int pos[2];                     // position of the thread's two rows; -1 where there is no row
-  long long item_first = first - at.unit;   // the item's first unit
+  int low = 0, high = 0;          // the lowest of them, the highest before the highest one's window
+  int began = 0;                  // the item's first unit, counted from the share's
   bool fresh = true;
-  int stage = 0;
-  for (long long u = 0; u < count; ++u) {
+  int stage = 0, seen = 0;        // stage and word of unit u
+  for (int u = 0; u < count; ++u) {
     if (fresh) {                  // a new item: its query rows
       fresh = false;
-      item_first = first + u - at.unit;
+      began = u - at.unit;
+      low = 0x7fffffff;
+      high = -0x7fffffff;
       const int r0 = at.tile * ROWS + wm * 16 + g;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = r0 + 8 * i;
         const bool ok = r < at.r.rows;
         pos[i] = ok ? at.r.length - at.r.n + r / p.group : -1;
+        if (ok) {
+          low = min(low, pos[i]);
+          high = max(high, pos[i] - p.window);
+        }
         const T* q = static_cast<const T*>(p.q) + (ok ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM : 0);
 #pragma unroll
         for (int s = 0; s < DIM / 16; ++s) {
@@ -187,15 +231,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
       for (int j = 0; j < DIM / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
     }
     copies_wait<kS - 2>();
+    publish();
     __syncthreads();
-    {
-      const int into = stage == 0 ? kS - 1 : stage - 1;
-      if (issued < count) {
-        copy_unit(into);
-        if (++issued < count) load.next(p);
-      }
-      copies_close();
-    }
+    copy_unit(stage == 0 ? kS - 1 : stage - 1);
     // ---- scores of this warp's keys ----
     const char* kbase = smem + stage * L::kStage;
     const char* vbase = kbase + kKeys * L::kRow;
@@ -219,37 +257,58 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
       }
     }
     // ---- running maxima and sums ----
-    const unsigned char* here = there + stage * kKeys + wk * kMine;
-    const float* sc = scales + stage * 3 * kKeys + wk * kMine;
+    const float* sc = scales + stage * 2 * kKeys + wk * kMine;
+    uint64_t see_all = (uint64_t)there[2 * seen + 1] << 32 | there[2 * seen];
+    see_all >>= wk * kMine;
+    const int key0 = at.key + wk * kMine;
+    // every row of the warp sees all of its keys
+    const bool clear = (kMine == 64 ? see_all == ~0ull : (see_all & ((1ull << (kMine & 63)) - 1)) == (1ull << (kMine & 63)) - 1) &&
+                       __all_sync(0xffffffffu, key0 + kMine - 1 <= low && (p.window == 0 || key0 > high));
     float best[2] = {top[0], top[1]};
 #pragma unroll
-    for (int j = 0; j < kMine / 8; ++j)
+    for (int j = 0; j < kMine / 8; ++j) {
+      float by[2] = {p.scale_log2, p.scale_log2};
+      [[maybe_unused]] float lift[2] = {0.f, 0.f};
+      if constexpr (k8) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          by[i] *= sc[j * 8 + 2 * tq + i];
+          lift[i] = exponent_of(sc[kKeys + j * 8 + 2 * tq + i]);
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int col = j * 8 + 2 * tq + (e & 1), key = at.key + wk * kMine + col, i = e >> 1;
-        const bool see = here[col] && key <= pos[i] && (p.window == 0 || key > pos[i] - p.window);
-        s[j][e] = see ? s[j][e] * (k8 ? sc[col] : p.scale_log2) : -INFINITY;
-        best[i] = fmaxf(best[i], k8 ? s[j][e] + sc[2 * kKeys + col] : s[j][e]);
+        const int col = j * 8 + 2 * tq + (e & 1), i = e >> 1;
+        s[j][e] *= by[e & 1];
+        if (!clear) {
+          const int key = key0 + col;
+          const bool see = (see_all >> col) & 1u && key <= pos[i] && (p.window == 0 || key > pos[i] - p.window);
+          s[j][e] = see ? s[j][e] : -INFINITY;
+        }
+        best[i] = fmaxf(best[i], k8 ? s[j][e] + lift[e & 1] : s[j][e]);
       }
+    }
     float safe[2], shrink[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 1));
       best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 2));
       safe[i] = best[i] == -INFINITY ? 0.f : best[i];
-      shrink[i] = exp2f(top[i] - safe[i]);
+      shrink[i] = ex2(top[i] - safe[i]);
       top[i] = best[i];
       sum[i] *= shrink[i];
     }
+    if (__any_sync(0xffffffffu, shrink[0] != 1.f || shrink[1] != 1.f)) {
 #pragma unroll
-    for (int j = 0; j < DIM / 8; ++j) { o[j][0] *= shrink[0]; o[j][1] *= shrink[0]; o[j][2] *= shrink[1]; o[j][3] *= shrink[1]; }
+      for (int j = 0; j < DIM / 8; ++j) { o[j][0] *= shrink[0]; o[j][1] *= shrink[0]; o[j][2] *= shrink[1]; o[j][3] *= shrink[1]; }
+    }
     uint32_t pf[kMine / 16][4];
 #pragma unroll
     for (int j = 0; j < kMine / 8; ++j) {
       float e[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        e[x] = exp2f(s[j][x] - safe[x >> 1]);
+        e[x] = ex2(s[j][x] - safe[x >> 1]);
         sum[x >> 1] += e[x];
         if constexpr (k8) e[x] *= sc[kKeys + j * 8 + 2 * tq + (x & 1)];
       }
@@ -282,7 +341,6 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
         }
       }
     }
-    stage = stage + 1 == kS ? 0 : stage + 1;
 
     // ---- the item's end, or the share's ----
     const bool last = at.unit + 1 == at.units;
@@ -292,41 +350,42 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
         sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
         sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
       }
-      // warps that shared the keys: the upper half hands its rows to the lower one, until one has all
-      constexpr int kPitch = DIM + 4;
+      // warps that shared the keys: the upper half hands its rows to the lower one, until one has all; through the unit's own
+      // stage, which takes no copies before the next barrier
 #pragma unroll
       for (int half = kWarpsK / 2; half > 0; half >>= 1) {
         __syncthreads();
-        float* box = join + (kWarpsK == 4 ? (wk & (half - 1)) : wm) * 16 * kPitch;
+        const int which = kWarpsK == 4 ? (wk & (half - 1)) : wm;
+        float* box = reinterpret_cast<float*>(smem + stage * L::kStage) + which * 16 * DIM;
         if (wk >= half && wk < 2 * half) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float* x = box + (g + 8 * i) * kPitch;
+            float* x = box + (g + 8 * i) * DIM;
 #pragma unroll
-            for (int j = 0; j < DIM / 8; ++j) *reinterpret_cast<float2*>(x + j * 8 + 2 * tq) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
-            if (tq == 0) *reinterpret_cast<float2*>(x + DIM) = make_float2(top[i], sum[i]);
+            for (int j = 0; j < DIM / 8; ++j) *reinterpret_cast<float2*>(x + ((j ^ g) * 8 + 2 * tq)) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
+            if (tq == 0) box_ts[which * 16 + g + 8 * i] = make_float2(top[i], sum[i]);
           }
         }
         __syncthreads();
         if (wk < half) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const float* x = box + (g + 8 * i) * kPitch;
-            const float2 ts = *reinterpret_cast<const float2*>(x + DIM);
+            const float* x = box + (g + 8 * i) * DIM;
+            const float2 ts = box_ts[which * 16 + g + 8 * i];
             const float both = fmaxf(top[i], ts.x), ref = both == -INFINITY ? 0.f : both;
-            const float a = exp2f(top[i] - ref), b = exp2f(ts.x - ref);
+            const float a = ex2(top[i] - ref), b = ex2(ts.x - ref);
             top[i] = both;
             sum[i] = sum[i] * a + ts.y * b;
 #pragma unroll
             for (int j = 0; j < DIM / 8; ++j) {
-              const float2 v = *reinterpret_cast<const float2*>(x + j * 8 + 2 * tq);
+              const float2 v = *reinterpret_cast<const float2*>(x + ((j ^ g) * 8 + 2 * tq));
               o[j][2 * i] = o[j][2 * i] * a + v.x * b;
               o[j][2 * i + 1] = o[j][2 * i + 1] * a + v.y * b;
             }
           }
         }
       }
-      const bool whole = last && item_first >= first;
+      const bool whole = last && began >= 0;
       if (wk == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -350,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
               if (p.lse && tq == 0)
                 p.lse[token * p.q_heads + qh] = 0.69314718055994531f * ((top[i] == -INFINITY ? 0.f : top[i]) + log2f(sum[i]));
             } else {
-              float* slot = p.part + (2 * share + (item_first >= first)) * (long long)(ROWS * (DIM + 2));
+              float* slot = p.part + (2 * share + (began >= 0)) * (long long)(ROWS * (DIM + 2));
               float* x = slot + in * DIM;
               if constexpr (k8) {
 #pragma unroll
@@ -369,14 +428,16 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
         }
       }
       if (u + 1 == count && tid == 0) {
-        const bool open = !last && item_first >= first;
-        const long long end = item_first + at.units - 1;       // the item's last unit
+        const bool open = !last && began >= 0;
+        const long long end = first + began + at.units - 1;    // the item's last unit
         p.open[2 * share] = make_int4(at.r.q0, at.h, at.tile * ROWS, min(ROWS, at.r.rows - at.tile * ROWS));
         p.open[2 * share + 1] = make_int4(open ? (int)(end / per) : -1, 0, 0, 0);
       }
       fresh = true;
     }
     if (u + 1 < count) at.next(p);
+    stage = stage + 1 == kS ? 0 : stage + 1;
+    seen = seen == kS ? 0 : seen + 1;
   }
   launch_dependents_now();
 }

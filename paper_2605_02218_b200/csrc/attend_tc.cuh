@@ -5,12 +5,16 @@
 // tiles; the probabilities overwrite S in 16 bits and are the A operand of the second product from there.  Keys are K-major, values
 // MN-major (keys are the inner dimension of the second product), both as rows of 64 features in 128-byte swizzled tiles.
 //
-// Warps: 0-3 and 4-7 softmax of tile 0 and 1, a row a thread; 8 issues the products; 9-12 bring queries, keys and values into
-// shared memory: 16-bit rows by asynchronous copies, 8-bit ones through registers, where they are widened (attend_kernels.cuh).
+// Warps: 0-3 and 4-7 softmax of tile 0 and 1, a row a thread; 8-10 bring queries, keys and values into shared memory, 16-bit rows by
+// asynchronous copies, 8-bit ones through registers, where they are widened (attend_kernels.cuh); 11 issues the products.  Twelve
+// warps leave each thread 168 registers; with 16 and registers moved between them, some of either kind spilled.
 //
-// The running maximum is only a reference that keeps the exponentials in range: a row whose scores stay within 2^8 of it keeps
-// it, so that O is rescaled seldom, and one pass over S makes the probabilities.  A warp with a row beyond that goes over S again.
+// The running maximum is only a reference that keeps the exponentials in range: a row keeps it
+// while a unit's probabilities add up to at most 2^14, so that O is rescaled seldom and one pass over S makes the probabilities.  A
+// warp with a row beyond that goes over S again with new references.
 #pragma once
+#include <type_traits>
+
 #include "attend_kernels.cuh"
 
 namespace covspec {
@@ -20,13 +24,14 @@ namespace wide {
 using namespace tc;
 
 constexpr int kRows = 256, kKeys = 128;
-constexpr int kThreads = 13 * 32;
-constexpr int kProducers = 128;
-constexpr float kSlack = 8.f;               // log2 of how far a score may lie above the reference
+constexpr int kThreads = 12 * 32;
+constexpr int kProducers = 96;
+constexpr float kMost = 16384.f;            // a unit's probabilities add up to no more over their reference
 
 template <int STORE, int DIM> struct Layout {
   static constexpr bool k8 = STORE >= cache::kE4M3;
   static constexpr int kSlot = kKeys * DIM * 2;                // keys or values of a unit, 16-bit
+  static constexpr int kRow = DIM * (k8 ? 1 : 2);              // bytes of a row in the cache
   static constexpr int kQ = kRows * DIM * 2;
   static constexpr int kSlots = k8 ? 4 : 5;
   static constexpr int kTail = 4 * 16                          // which keys of a unit are there, 4 units
@@ -38,11 +43,6 @@ template <int STORE, int DIM> struct Layout {
   static_assert(kSmem <= 232448);
 };
 
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 template <typename T> __device__ __forceinline__ uint32_t idesc(int n, bool b_mn) {
   const uint32_t type = __is_same(T, __half) ? 0u : 1u;
   return (1u << 4) | (type << 7) | (type << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -80,6 +80,26 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 16 columns of this warp's lanes; the registers hold them after tmem_arrived on them.
+__device__ __forceinline__ void tmem_fetch(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
+
 // Barrier among `n` threads that tells each whether all came with `v`.
 __device__ __forceinline__ bool barrier_and(int id, int n, bool v) {
   uint32_t r;
@@ -110,8 +130,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
   uint8_t* tail = ring + kSlots * L::kSlot;
   uint32_t* there = reinterpret_cast<uint32_t*>(tail);                       // [4][4]
   float* scales = reinterpret_cast<float*>(tail + 64);                       // [4][2][kKeys]: key scale * scale_log2, value scale
-  int2* places = reinterpret_cast<int2*>(tail + 64 + (k8 ? 4 * 2 * kKeys * 4 : 0));   // [2][kKeys]: page (-1: none), row in it
-  uint64_t* bars = reinterpret_cast<uint64_t*>(places + 2 * kKeys);
+  uint32_t* places = reinterpret_cast<uint32_t*>(tail + 64 + (k8 ? 4 * 2 * kKeys * 4 : 0));  // [2][2][kKeys]: keys', values' rows in 16 bytes
+  uint64_t* bars = reinterpret_cast<uint64_t*>(places + 4 * kKeys);
   uint64_t *full = bars, *empty = bars + 5, *q_full = bars + 10, *q_empty = bars + 11, *s_full = bars + 12, *p_ready = bars + 14,
            *o_full = bars + 16, *drained = bars + 18;                        // 19 barriers
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
@@ -129,23 +149,23 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
   wait_for_previous_kernel();
   Cursor<kRows, kKeys> at;
   long long first, per;
-  const long long count = find_share<kRows, kKeys, kThreads>(p, at, first, per, reinterpret_cast<long long*>(places));
-  const long long share = blockIdx.x;
+  const int count = find_share<kRows, kKeys, kThreads>(p, at, first, per, reinterpret_cast<long long*>(places));
+  const int share = blockIdx.x;
   if (count <= 0) {
     if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
     launch_dependents_now();
     return;
   }
-  if (warp == 8) tmem_alloc(tmem_slot, 512);
+  if (warp == 11) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   constexpr uint32_t kO = 256;                                 // first column of O; tile x: S at 128 x, O at kO + 128 x
 
-  if (warp >= 9) {
+  if (warp >= 8 && warp < 11) {
     // ---------------- producers ----------------
-    const int t = tid - 9 * 32;
+    const int t = tid - 8 * 32, wp = warp - 8;
     uint64_t* waiting[3] = {nullptr, nullptr, nullptr};        // barriers of copies that are under way, the oldest last
     auto close = [&](uint64_t* bar) {                          // the copies so far belong to `bar`
       copies_close();
@@ -173,15 +193,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
     uint32_t phase = 1, q_phase = 1;
     bool ok = true, fresh = true;
     auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
-    for (long long u = 0; u < count; ++u) {
-      if (fresh) {
-        fresh = false;
+    int page[2] = {-1, -1};
+    auto look_up = [&] {                                       // pages of this thread's keys of the unit at `at`
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int key = at.key + t + i * kProducers;
+        const bool mine = (i == 0 || wp == 0) && key >= at.k.lo && key < at.k.hi;
+        page[i] = mine ? p.t.table[at.b * p.t.table_ld + (key >> p.c.page_shift)] : -1;
+      }
+    };
+    auto spot_of = [&](long long page_ld, int page, int row) {
+      return (uint32_t)((unsigned long long)(page * page_ld + (long long)row * DIM) / (16 / (L::kRow / DIM)));
+    };
+    look_up();
+    for (int u = 0; u < count; ++u) {
+      if (fresh) {                                             // `at` is at unit u here: its queries
         ok = ok && acquire(q_empty, q_phase);
         q_phase ^= 1u;
-        constexpr int kChunks = DIM / 8;
-        const int chunk = t % kChunks;
+        constexpr int kChunks = DIM / 8, kAtOnce = 32 / kChunks;
+        const int chunk = lane % kChunks;
 #pragma unroll 4
-        for (int row = t / kChunks; row < kRows; row += kProducers / kChunks) {
+        for (int row = wp * kAtOnce + lane / kChunks; row < kRows; row += 3 * kAtOnce) {
           const int r = at.tile * kRows + row;
           const bool there_is = ok && r < at.r.rows;
           const T* q = static_cast<const T*>(p.q) +
@@ -190,25 +222,46 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         }
         close(q_full);
       }
-      // places of the unit's keys, a key a thread
-      int2* place = places + (u & 1) * kKeys;
+      // places of the unit's keys: a thread has key t, the first warp the last 32 too; the pages of the next unit's keys are under
+      // way meanwhile
+      uint32_t* place = places + (u & 1) * 2 * kKeys;
       {
-        const int key = at.key + t;
-        int page = -1;
-        if (key >= at.k.lo && key < at.k.hi) page = p.t.table[at.b * p.t.table_ld + (key >> p.c.page_shift)];
-        const bool is = (unsigned)page < (unsigned)p.c.pages;
-        const int row = (at.h << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1));
+        uint2 spot[2];
+        bool is[2];
+        [[maybe_unused]] float ks[2] = {0.f, 0.f}, vs[2] = {1.f, 1.f};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = (at.h << p.c.page_shift) + ((at.key + t + i * kProducers) & ((1 << p.c.page_shift) - 1));
+          is[i] = (unsigned)page[i] < (unsigned)p.c.pages;
+          spot[i] = is[i] ? make_uint2(spot_of(p.c.k_page, page[i], row), spot_of(p.c.v_page, page[i], row)) : make_uint2(kNowhere, kNowhere);
+          if constexpr (k8) {
+            const long long w = (((long long)page[i] * p.c.heads) << p.c.page_shift) + row;
+            if (is[i]) {
+              ks[i] = p.c.k_scale[w] * p.scale_log2;
+              vs[i] = p.c.v_scale[w];
+            }
+          }
+        }
+        fresh = at.unit + 1 == at.units;
+        if (u + 1 < count) {
+          at.next(p);
+          look_up();
+        }
         // the words of unit u - 4 have been read: its products are done (the slot that this unit's keys take says so)
         ok = ok && acquire(empty + slot, phase);
-        place[t] = make_int2(is ? page : -1, row);
-        const uint32_t word = __ballot_sync(0xffffffffu, is);
-        if (lane == 0) there[(u & 3) * 4 + (t >> 5)] = word;
-        if constexpr (k8) {
-          float* sc = scales + (u & 3) * 2 * kKeys;
-          const long long w = (((long long)page * p.c.heads) << p.c.page_shift) + row;
-          const float vs = is ? p.c.v_scale[w] : 1.f;
-          sc[t] = is ? p.c.k_scale[w] * p.scale_log2 : 0.f;
-          sc[kKeys + t] = vs < cache::kLeastScale ? cache::kLeastScale : vs;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int key = t + i * kProducers;
+          if (i == 1 && wp != 0) break;
+          place[key] = spot[i].x;
+          place[kKeys + key] = spot[i].y;
+          const uint32_t word = __ballot_sync(0xffffffffu, is[i]);
+          if (lane == 0) there[(u & 3) * 4 + (key >> 5)] = word;
+          if constexpr (k8) {
+            float* sc = scales + (u & 3) * 2 * kKeys;
+            sc[key] = ks[i];
+            sc[kKeys + key] = vs[i] < cache::kLeastScale ? cache::kLeastScale : vs[i];
+          }
         }
       }
       // all of them go on or none: a thread that has left would be waited for at the next barrier
@@ -217,31 +270,31 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
       for (int kv = 0; kv < 2; ++kv) {
         if (kv && !(ok = acquire(empty + slot, phase))) break;
         uint8_t* dst = ring + slot * L::kSlot;
-        const char* base = static_cast<const char*>(kv ? p.c.v : p.c.k);
-        const long long page_ld = kv ? p.c.v_page : p.c.k_page;
+        constexpr int kChunks = L::kRow / 16, kAtOnce = 32 / kChunks, kPer = (kKeys / kAtOnce + 2) / 3;
+        const int chunk = lane % kChunks;
+        const char* base = static_cast<const char*>(kv ? p.c.v : p.c.k) + chunk * 16;
+        auto row_of = [&](int i) { return (wp + 3 * i) * kAtOnce + lane / kChunks; };
+        uint32_t spot[kPer];                                   // read ahead: no load passes a copy
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) spot[i] = row_of(i) < kKeys ? place[kv * kKeys + row_of(i)] : kNowhere;
         if constexpr (!k8) {
-          constexpr int kChunks = DIM / 8, kStep = kProducers / kChunks;
-          const int chunk = t % kChunks;
-#pragma unroll 4
-          for (int row = t / kChunks; row < kKeys; row += kStep) {
-            const int2 pl = place[row];
-            const bool is = pl.x >= 0;
-            const char* src = base + (is ? (pl.x * page_ld + (long long)pl.y * DIM) * 2 + chunk * 16 : 0);
-            copy16(smem_u32(dst + tile_at(kKeys, row, chunk)), src, is);
+          const uint32_t to = smem_u32(dst);
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const bool is = spot[i] != kNowhere;
+            if (i < kPer - 1 || row_of(i) < kKeys)
+              copy16(to + tile_at(kKeys, row_of(i), chunk), base + (is ? (unsigned long long)spot[i] * 16 : 0ull), is);
           }
           close(full + slot);
         } else {
-          constexpr int kChunks = DIM / 16, kStep = kProducers / kChunks, kPer = kKeys / kStep;
-          const int chunk = t % kChunks;
           uint4 raw[kPer];
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) {
-            const int2 pl = place[t / kChunks + i * kStep];
-            raw[i] = pl.x >= 0 ? *reinterpret_cast<const uint4*>(base + pl.x * page_ld + (long long)pl.y * DIM + chunk * 16) : make_uint4(0u, 0u, 0u, 0u);
-          }
+          for (int i = 0; i < kPer; ++i)
+            raw[i] = spot[i] != kNowhere ? *reinterpret_cast<const uint4*>(base + (unsigned long long)spot[i] * 16) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
           for (int i = 0; i < kPer; ++i) {
-            const int row = t / kChunks + i * kStep;
+            const int row = row_of(i);
+            if (i == kPer - 1 && row >= kKeys) break;
             const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
             uint32_t v[8];
 #pragma unroll
@@ -257,13 +310,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         }
         next_slot();
       }
-      if (u + 1 < count) {
-        fresh = at.unit + 1 == at.units;
-        at.next(p);
-      }
     }
     flush();
-  } else if (warp == 8) {
+  } else if (warp == 11) {
     // ---------------- products ----------------
     const uint32_t qk = idesc<T>(kKeys, false), pv = idesc<T>(DIM, true);
     int k_slot = 0, slot = 0;                                  // slot of the keys in S, next slot of the ring
@@ -287,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         mma_ts(tmem + kO + x * 128, tmem + x * 128 + 8 * k, b + k * (16 * 128 / 16), pv, accumulate || k != 0);
     };
     bool fresh = true, opened = false;                         // the next unit begins an item; its scores are issued
-    for (long long u = 0; u < count && ok; ++u) {
+    for (int u = 0; u < count && ok; ++u) {
       const bool two = at.r.rows - at.tile * kRows > 128;
       const bool begins = fresh;
       if (!opened) {
@@ -355,14 +404,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
     const uint32_t s_at = tmem + x * 128 + ((uint32_t)(warp & 3) << 21), o_at = s_at + kO;
     float ref = 0.f, sum = 0.f;
     int pos = -1;
-    long long item_first = 0;
+    int began = 0;                                             // the item's first unit, counted from the share's
     bool fresh = true, ok = true, active = false;
     uint32_t s_phase = 0, o_phase = 0;
-    for (long long u = 0; u < count; ++u) {
+    for (int u = 0; u < count; ++u) {
       const int r = at.tile * kRows + x * 128 + row;
       if (fresh) {
         fresh = false;
-        item_first = first + u - at.unit;
+        began = u - at.unit;
         active = at.r.rows - at.tile * kRows > x * 128;
         const bool is = r < at.r.rows;
         pos = is ? at.r.length - at.r.n + r / p.group : -1;
@@ -379,77 +428,86 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         const bool clear = (bits.x & bits.y & bits.z & bits.w) == 0xffffffffu &&
                            __all_sync(0xffffffffu, pos < 0 ? r >= at.r.rows : at.key + kKeys - 1 <= pos && (p.window == 0 || at.key > pos - p.window));
         const int lowest = p.window ? max(pos - p.window + 1, 0) : 0;
-        // scores of 32 keys: scaled, those not seen -inf
-        auto fetch = [&](int c, float (&v)[32]) {
-          tmem_ld32(s_at + 32 * c, v);
-          if constexpr (k8) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float4 a = *reinterpret_cast<const float4*>(sc + 32 * c + e);
-              v[e] *= a.x; v[e + 1] *= a.y; v[e + 2] *= a.z; v[e + 3] *= a.w;
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] *= p.scale_log2;
-          }
-          if (!clear) {
-            const uint32_t word = c == 0 ? bits.x : c == 1 ? bits.y : c == 2 ? bits.z : bits.w;
-            const int k0 = at.key + 32 * c;
-            // bits of the keys lowest .. pos
-            uint32_t see = word;
-            see &= pos < k0 ? 0u : pos - k0 >= 31 ? 0xffffffffu : (2u << (pos - k0)) - 1u;
-            see &= lowest <= k0 ? 0xffffffffu : lowest - k0 > 31 ? 0u : ~((1u << (lowest - k0)) - 1u);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : -INFINITY;
-          }
+        // bits of 32 keys that the row sees
+        auto seen = [&](int c) {
+          const int k0 = at.key + 32 * c;
+          uint32_t see = c == 0 ? bits.x : c == 1 ? bits.y : c == 2 ? bits.z : bits.w;
+          see &= pos < k0 ? 0u : pos - k0 >= 31 ? 0xffffffffu : (2u << (pos - k0)) - 1u;
+          see &= lowest <= k0 ? 0xffffffffu : lowest - k0 > 31 ? 0u : ~((1u << (lowest - k0)) - 1u);
+          return see;
         };
         uint32_t packed[64];
-        float top = 0.f, more = 0.f;
-        auto make = [&](float safe) {
-          top = -INFINITY;
-          more = 0.f;
+        float more = 0.f, most = 0.f;                          // sums of the probabilities, without and with the values' scales
+        auto make = [&](float safe, auto masked) {
+          const f32x2 low = pack2(-safe, -safe), by = pack2(p.scale_log2, p.scale_log2);
+          f32x2 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)}, most2 = pack2(0.f, 0.f);
+          uint32_t v[2][16];
+          tmem_fetch(s_at, v[0]);
+          tmem_arrived(v[0]);
+          uint32_t see = 0;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float v[32];
-            fetch(c, v);
+          for (int c = 0; c < 8; ++c) {
+            if (c < 7) tmem_fetch(s_at + 16 * (c + 1), v[(c + 1) & 1]);
+            const uint32_t (&w)[16] = v[c & 1];
+            if constexpr (decltype(masked)::value) see = c & 1 ? see >> 16 : seen(c / 2);
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                v[e + i] = ex2(v[e + i] - safe);
-                more += v[e + i];
-              }
+            for (int e = 0; e < 16; e += 4) {
+              f32x2 f[2] = {by, by};
+              [[maybe_unused]] f32x2 g[2] = {by, by};
               if constexpr (k8) {
-                const float4 w = *reinterpret_cast<const float4*>(sc + kKeys + 32 * c + e);
-                v[e] *= w.x; v[e + 1] *= w.y; v[e + 2] *= w.z; v[e + 3] *= w.w;
+                const float4 a = *reinterpret_cast<const float4*>(sc + 16 * c + e), b = *reinterpret_cast<const float4*>(sc + kKeys + 16 * c + e);
+                f[0] = pack2(a.x, a.y); f[1] = pack2(a.z, a.w);
+                g[0] = pack2(b.x, b.y); g[1] = pack2(b.z, b.w);
               }
 #pragma unroll
-              for (int i = 0; i < 4; ++i) top = fmaxf(top, v[e + i]);
-              packed[16 * c + e / 2] = pack2of<T>(v[e], v[e + 1]);
-              packed[16 * c + e / 2 + 1] = pack2of<T>(v[e + 2], v[e + 3]);
+              for (int i = 0; i < 2; ++i) {
+                float2 t = unpack2(fma2(pack2(__uint_as_float(w[e + 2 * i]), __uint_as_float(w[e + 2 * i + 1])), f[i], low));
+                if constexpr (decltype(masked)::value) {
+                  t.x = (see >> (e + 2 * i)) & 1u ? t.x : -INFINITY;
+                  t.y = (see >> (e + 2 * i + 1)) & 1u ? t.y : -INFINITY;
+                }
+                t.x = ex2(t.x);
+                t.y = ex2(t.y);
+                f32x2 t2 = pack2(t.x, t.y);
+                sum2[i] = add2(sum2[i], t2);
+                if constexpr (k8) {
+                  t2 = mul2(t2, g[i]);
+                  most2 = add2(most2, t2);
+                  t = unpack2(t2);
+                }
+                packed[8 * c + e / 2 + i] = pack2of<T>(t.x, t.y);
+              }
             }
+            if (c < 7) tmem_arrived(v[(c + 1) & 1]);
           }
+          const float2 a = unpack2(add2(sum2[0], sum2[1])), b = unpack2(most2);
+          more = a.x + a.y;
+          most = k8 ? b.x + b.y : more;
         };
-        const bool unset = ref == -INFINITY;
-        bool again = __any_sync(0xffffffffu, unset);
+        bool again = __any_sync(0xffffffffu, ref == -INFINITY);
         if (!again) {
-          make(ref);
-          again = __any_sync(0xffffffffu, top > 256.f);
+          if (clear) make(ref, std::false_type());
+          else make(ref, std::true_type());
+          again = __any_sync(0xffffffffu, most > kMost);
         }
         if (again) {                                           // new references, from the scores themselves
           float best = ref;
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            float v[32];
-            fetch(c, v);
+          for (int c = 0; c < 8; ++c) {
+            float v[16];
+            tmem_ld16(s_at + 16 * c, v);
+            const uint32_t see = seen(c / 2) >> (16 * (c & 1));
 #pragma unroll
-            for (int e = 0; e < 32; ++e) best = fmaxf(best, k8 ? v[e] + log2f(sc[kKeys + 32 * c + e]) : v[e]);
+            for (int e = 0; e < 16; ++e) {
+              const int key = 16 * c + e;
+              const float t = k8 ? v[e] * sc[key] + log2f(sc[kKeys + key]) : v[e] * p.scale_log2;
+              best = (see >> e) & 1u ? fmaxf(best, t) : best;
+            }
           }
-          const float old = ref;
-          if (best > ref) ref = best;
-          const float shrink = old == -INFINITY ? 0.f : ex2(old - ref);
+          const float shrink = ref == -INFINITY ? 0.f : ex2(ref - best);
+          ref = best;
           sum *= shrink;
-          if (first + u > max(item_first, first)) {            // O holds earlier units' rows
+          if (u > max(began, 0)) {                             // O holds earlier units' rows
 #pragma unroll 1
             for (int c = 0; c < DIM / 32; ++c) {
               float v[32];
@@ -461,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
             }
             tmem_st_wait();
           }
-          make(ref == -INFINITY ? 0.f : ref);
+          make(ref == -INFINITY ? 0.f : ref, std::true_type());
         }
         sum += more;
         tmem_st32(s_at, packed);
@@ -473,7 +531,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
       }
       const bool last = at.unit + 1 == at.units;
       if (last || u + 1 == count) {
-        const bool whole = last && item_first >= first;
+        const bool whole = last && began >= 0;
         if (active) {
           ok = ok && mbar_wait(o_full + x, o_phase, abort_flag);
           o_phase ^= 1u;
@@ -484,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
           const long long token = is ? token_of(p, at.r.q0, r) : 0;
           const int qh = is ? head_of(p, at.h, r) : 0;
           T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM;
-          float* slot = p.part + (2 * share + (item_first >= first)) * (long long)(kRows * (DIM + 2));
+          float* slot = p.part + (2 * share + (began >= 0)) * (long long)(kRows * (DIM + 2));
           const int in = x * 128 + row;
 #pragma unroll 1
           for (int c = 0; c < DIM / 32; ++c) {
@@ -512,8 +570,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
           tc_fence_before();
         }
         if (u + 1 == count && tid == 0) {
-          const bool open = !last && item_first >= first;
-          const long long end = item_first + at.units - 1;
+          const bool open = !last && began >= 0;
+          const long long end = first + began + at.units - 1;
           p.open[2 * share] = make_int4(at.r.q0, at.h, at.tile * kRows, min(kRows, at.r.rows - at.tile * kRows));
           p.open[2 * share + 1] = make_int4(open ? (int)(end / per) : -1, 0, 0, 0);
         }
@@ -525,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (warp == 11) tmem_dealloc(tmem, 512);
   launch_dependents_now();
 }
 

@@ -92,23 +92,75 @@ __device__ __forceinline__ float quotient_sticky(float x, float s) {
   const float rest = fmaf(-t, s, x);
   return rest != 0.f ? __uint_as_float(__float_as_uint(t) | 1u) : t;
 }
-
-// The 8-bit form of eight values, as the bytes of a uint2.
+// The 8-bit form of eight values, as the bytes of a uint2.  t = x times the rounded 1 / s is off by less than 2^-22 of the quotient;
+// what decides next to a border between two held values is the exact rest x - border * s.  Quotients of 16-bit numbers meet
+// borders all the time (half of the largest value is 63.5 steps of int8), so the rest costs no division: with one for each
+// value 27.8 k tokens x 8 heads x 128 features took 132 us, and with one where it is close 178.
+//  int8: the rest of the nearest step k, a multiple of half a unit in the last place of s below s, is exact in float32.
+//  e4m3: 20 of the 23 bits go, a border is a half of the last that stays; below the normal numbers the quotient itself is taken.
 template <int STORE>
 __device__ __forceinline__ uint2 held8(const float (&x)[8], float s) {
+  const float inv = __frcp_rn(s), half = 0.5f * s;
   uint2 r = make_uint2(0u, 0u);
+  if constexpr (STORE == kInt8) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = quotient_sticky(x[i], s);
-    unsigned byte;
-    if constexpr (STORE == kE4M3) {
-      byte = __nv_cvt_float_to_fp8(t, __NV_SATFINITE, __NV_E4M3);
-    } else {
-      byte = (unsigned)max(-127, min(127, __float2int_rn(t))) & 0xffu;
+    for (int i = 0; i < 8; ++i) {
+      constexpr float kMagic = 12582912.f;           // 1.5 * 2^23: the sum's last bits are the rounded number
+      const float m = x[i] * inv + kMagic, k = m - kMagic, rest = fmaf(-k, s, x[i]);
+      int held = (int)__float_as_uint(m);
+      if (fabsf(rest) >= half && (fabsf(rest) > half || (held & 1))) held += rest > 0.f ? 1 : -1;
+      (i < 4 ? r.x : r.y) |= ((unsigned)held & 0xffu) << (8 * (i & 3));
     }
-    (i < 4 ? r.x : r.y) |= byte << (8 * (i & 3));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      float t[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float v = x[i + j];
+        t[j] = v * inv;
+        const uint32_t bits = __float_as_uint(t[j]);
+        if (((bits + 8u) & 0xfffffu) - 0x80000u <= 16u) {
+          const uint32_t border = (bits + 8u) & 0xfff00000u | 0x80000u;
+          const float rest = fmaf(-__uint_as_float(border), s, v);
+          t[j] = __uint_as_float(rest == 0.f ? border : (rest > 0.f) == (v > 0.f) ? border + 1u : border - 1u);
+        }
+        if (fabsf(t[j]) < 0.015625f && v != 0.f) t[j] = quotient_sticky(v, s);
+      }
+      const unsigned two = __nv_cvt_float2_to_fp8x2(make_float2(t[0], t[1]), __NV_SATFINITE, __NV_E4M3);
+      (i < 4 ? r.x : r.y) |= two << (8 * (i & 3));
+    }
   }
   return r;
+}
+
+// A warp takes kPasses times as many neighbouring (token, head) rows as its lanes cover with 16 bytes each.  Every lane finds the
+// place of one row, so the chain of look-ups (request, length, page) is gone through once per warp, then all rows' loads are in
+// flight together.
+constexpr int kPasses = 4;
+struct Spot {
+  int page, row, source;       // page -1: none; row (head * page_size + place) in it; row of the dense side
+};
+__device__ __forceinline__ Spot spot_of(const Tokens& t, const Pages& c, long long unit, int n, const int* rows, const int* row_offsets,
+                                        int source_rows) {
+  Spot s{-1, 0, -1};
+  const long long i64 = unit / c.heads;
+  if (i64 >= n) return s;
+  const int i = (int)i64, head = (int)(unit % c.heads), b = request_of(t, i);
+  if (b < 0) return s;
+  int place;
+  s.page = page_of(t, c, b, i, place);
+  s.row = (head << c.page_shift) + place;
+  s.source = i;
+  if (rows) {
+    const long long source = (long long)row_offsets[b] + rows[i];
+    if (source < 0 || source >= source_rows) s.page = -1;
+    s.source = (int)source;
+  }
+  return s;
+}
+__device__ __forceinline__ Spot handed(const Spot& s, int lane) {
+  return Spot{__shfl_sync(0xffffffffu, s.page, lane), __shfl_sync(0xffffffffu, s.row, lane), __shfl_sync(0xffffffffu, s.source, lane)};
 }
 
 struct WriteParams {
@@ -122,61 +174,60 @@ struct WriteParams {
   int source_rows;
 };
 
-// dim / 8 lanes per (token, head): one 16-byte load of the key's and one of the value's row per lane (two each for float32).
+// Eight features a lane: one 16-byte load (two for float32).
 template <typename T, int STORE, int DIM>
 __global__ void __launch_bounds__(kThreads) write_kernel(WriteParams p) {
-  constexpr int kLanes = DIM / 8;
-  const long long unit = ((long long)blockIdx.x * kThreads + threadIdx.x) / kLanes;
-  const int lane = threadIdx.x % kLanes;
-  const int i = (int)min(unit / p.c.heads, (long long)p.n), head = (int)(unit % p.c.heads);
-  int page = -1, place = 0;
-  long long source = i;
-  if (i < p.n) {
-    const int b = request_of(p.t, i);
-    if (b >= 0) {
-      page = page_of(p.t, p.c, b, i, place);
-      if (p.rows) {
-        source = (long long)p.row_offsets[b] + p.rows[i];
-        if (source < 0 || source >= p.source_rows) page = -1;
+  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes, kAtOnce = 2;
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, feature = lane % kLanes * 8;
+  const long long unit0 = ((long long)blockIdx.x * (kThreads / 32) + warp_index()) * (kRows * kPasses);
+  Spot mine = lane < kRows * kPasses ? spot_of(p.t, p.c, unit0 + lane, p.n, p.rows, p.row_offsets, p.source_rows) : Spot{-1, 0, -1};
+#pragma unroll
+  for (int first = 0; first < kPasses; first += kAtOnce) {
+    float x[kAtOnce][2][8];
+    Spot s[kAtOnce];
+#pragma unroll
+    for (int a = 0; a < kAtOnce; ++a) {
+      const int r = (first + a) * kRows + sub;
+      s[a] = handed(mine, r);
+      const int head = (int)((unit0 + r) % p.c.heads);
+      if (s[a].page >= 0) {
+        load8f(static_cast<const T*>(p.k) + s[a].source * p.k_ld + head * DIM + feature, x[a][0]);
+        load8f(static_cast<const T*>(p.v) + s[a].source * p.v_ld + head * DIM + feature, x[a][1]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[a][0][e] = x[a][1][e] = 0.f;
       }
     }
-  }
-  float x[2][8];
-  if (page >= 0) {
-    load8f(static_cast<const T*>(p.k) + source * p.k_ld + head * DIM + lane * 8, x[0]);
-    load8f(static_cast<const T*>(p.v) + source * p.v_ld + head * DIM + lane * 8, x[1]);
-  } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[0][e] = x[1][e] = 0.f;
-  }
-  const int row = (head << p.c.page_shift) + place;
+    for (int a = 0; a < kAtOnce; ++a)
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    void* base = kv ? p.c.v : p.c.k;
-    const long long at = page * (kv ? p.c.v_page : p.c.k_page) + (long long)row * DIM + lane * 8;
-    if constexpr (STORE >= kE4M3) {
-      float top = 0.f;
-      bool bad = false;
+      for (int kv = 0; kv < 2; ++kv) {
+        const int page = s[a].page;
+        void* base = kv ? p.c.v : p.c.k;
+        const long long at = page * (kv ? p.c.v_page : p.c.k_page) + (long long)s[a].row * DIM + feature;
+        if constexpr (STORE >= kE4M3) {
+          float top = 0.f;
+          bool bad = false;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        top = fmaxf(top, fabsf(x[kv][e]));
-        bad |= !(fabsf(x[kv][e]) <= 3.402823466e38f);
+          for (int e = 0; e < 8; ++e) {
+            top = fmaxf(top, fabsf(x[a][kv][e]));
+            bad |= x[a][kv][e] != x[a][kv][e];
+          }
+          if (bad) top = INFINITY;
+#pragma unroll
+          for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const bool finite = top <= 3.402823466e38f;
+          const float scale = finite ? fmaxf(__fdiv_rn(top, STORE == kE4M3 ? 448.f : 127.f), kLeastScale) : __int_as_float(0x7fffffff);
+          if (page >= 0) {
+            *reinterpret_cast<uint2*>(static_cast<unsigned char*>(base) + at) = finite ? held8<STORE>(x[a][kv], scale) : make_uint2(0u, 0u);
+            if (feature == 0) (kv ? p.c.v_scale : p.c.k_scale)[(((long long)page * p.c.heads) << p.c.page_shift) + s[a].row] = scale;
+          }
+        } else if (page >= 0) {
+          if constexpr (STORE == kF32) store8f(static_cast<float*>(base) + at, x[a][kv]);
+          else if constexpr (STORE == kBF16) store8f(static_cast<__nv_bfloat16*>(base) + at, x[a][kv]);
+          else store8f(static_cast<__half*>(base) + at, x[a][kv]);
+        }
       }
-      if (bad) top = INFINITY;
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const bool finite = top <= 3.402823466e38f;
-      const float s = finite ? fmaxf(__fdiv_rn(top, STORE == kE4M3 ? 448.f : 127.f), kLeastScale) : __int_as_float(0x7fffffff);
-      if (page >= 0) {
-        const uint2 held = finite ? held8<STORE>(x[kv], s) : make_uint2(0u, 0u);
-        *reinterpret_cast<uint2*>(static_cast<unsigned char*>(base) + at) = held;
-        if (lane == 0) (kv ? p.c.v_scale : p.c.k_scale)[(((long long)page * p.c.heads) << p.c.page_shift) + row] = s;
-      }
-    } else if (page >= 0) {
-      if constexpr (STORE == kF32) store8f(static_cast<float*>(base) + at, x[kv]);
-      else if constexpr (STORE == kBF16) store8f(static_cast<__nv_bfloat16*>(base) + at, x[kv]);
-      else store8f(static_cast<__half*>(base) + at, x[kv]);
-    }
   }
 }
 
@@ -187,48 +238,78 @@ struct ReadParams {
   int n;
 };
 
-template <typename T, int STORE, int DIM>
-__global__ void __launch_bounds__(kThreads) read_kernel(ReadParams p) {
-  constexpr int kLanes = DIM / 8;
-  const long long unit = ((long long)blockIdx.x * kThreads + threadIdx.x) / kLanes;
-  const int lane = threadIdx.x % kLanes;
-  const int i = (int)min(unit / p.c.heads, (long long)p.n), head = (int)(unit % p.c.heads);
-  if (i >= p.n) return;
-  const int b = request_of(p.t, i);
-  if (b < 0) return;
-  int place;
-  const int page = page_of(p.t, p.c, b, i, place);
-  const int row = (head << p.c.page_shift) + place;
+// 16 bytes of the cache a lane, as E floats.
+template <int STORE, int E> __device__ __forceinline__ void widen_held(const uint4& h, float s, float (&x)[E]) {
+  const unsigned w[4] = {h.x, h.y, h.z, h.w};
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    float x[8];
-    if (page >= 0) {
-      const void* base = kv ? p.c.v : p.c.k;
-      const long long at = page * (kv ? p.c.v_page : p.c.k_page) + (long long)row * DIM + lane * 8;
-      if constexpr (STORE >= kE4M3) {
-        const uint2 h = *reinterpret_cast<const uint2*>(static_cast<const unsigned char*>(base) + at);
-        const float s = (kv ? p.c.v_scale : p.c.k_scale)[(((long long)page * p.c.heads) << p.c.page_shift) + row];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const unsigned byte = ((e < 4 ? h.x : h.y) >> (8 * (e & 3))) & 0xffu;
-          if constexpr (STORE == kE4M3) {
-            x[e] = s * __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
-          } else {
-            x[e] = s * (float)(signed char)byte;
-          }
-        }
-      } else if constexpr (STORE == kF32) {
-        load8f(static_cast<const float*>(base) + at, x);
-      } else if constexpr (STORE == kBF16) {
-        load8f(static_cast<const __nv_bfloat16*>(base) + at, x);
-      } else {
-        load8f(static_cast<const __half*>(base) + at, x);
-      }
+  for (int e = 0; e < E; ++e) {
+    if constexpr (STORE == kE4M3) {
+      x[e] = s * __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)((w[e / 4] >> (8 * (e & 3))) & 0xffu), __NV_E4M3)));
+    } else if constexpr (STORE == kInt8) {
+      x[e] = s * (float)(signed char)((w[e / 4] >> (8 * (e & 3))) & 0xffu);
+    } else if constexpr (STORE == kBF16) {
+      x[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    } else if constexpr (STORE == kF16) {
+      x[e] = __half2float(__ushort_as_half((unsigned short)(w[e / 2] >> (16 * (e & 1)))));
+    } else {
+      x[e] = __uint_as_float(w[e]);
+    }
+  }
+}
+template <typename T, int E> __device__ __forceinline__ void store_row(T* p, const float (&x)[E]) {
+  if constexpr (E == 4) {
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (__is_same(T, __half)) p[e] = __float2half_rn(x[e]);
+        else p[e] = __float2bfloat16_rn(x[e]);
+      }
     }
-    store8f(static_cast<T*>(kv ? p.v : p.k) + ((long long)i * p.c.heads + head) * DIM + lane * 8, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; i += 8) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = x[i + e];
+      store8f(p + i, y);
+    }
+  }
+}
+
+template <typename T, int STORE, int DIM>
+__global__ void __launch_bounds__(kThreads) read_kernel(ReadParams p) {
+  constexpr int E = STORE >= kE4M3 ? 16 : STORE == kF32 ? 4 : 8, kBytes = 16 / E;
+  constexpr int kLanes = DIM / E, kRows = 32 / kLanes;
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, feature = lane % kLanes * E;
+  const long long unit0 = ((long long)blockIdx.x * (kThreads / 32) + warp_index()) * (kRows * kPasses);
+  Spot mine = lane < kRows * kPasses ? spot_of(p.t, p.c, unit0 + lane, p.n, nullptr, nullptr, 0) : Spot{-1, 0, -1};
+  uint4 h[kPasses][2];
+  [[maybe_unused]] float scale[kPasses][2];
+#pragma unroll
+  for (int a = 0; a < kPasses; ++a) {
+    const Spot s = handed(mine, a * kRows + sub);
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      h[a][kv] = make_uint4(0u, 0u, 0u, 0u);
+      scale[a][kv] = 0.f;
+      if (s.page >= 0) {
+        const char* base = static_cast<const char*>(kv ? p.c.v : p.c.k);
+        h[a][kv] = *reinterpret_cast<const uint4*>(base + (s.page * (kv ? p.c.v_page : p.c.k_page) + (long long)s.row * DIM + feature) * kBytes);
+        if constexpr (STORE >= kE4M3) scale[a][kv] = (kv ? p.c.v_scale : p.c.k_scale)[(((long long)s.page * p.c.heads) << p.c.page_shift) + s.row];
+      }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < kPasses; ++a) {
+    if (__shfl_sync(0xffffffffu, mine.source, a * kRows + sub) < 0) continue;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      float x[E];
+      widen_held<STORE, E>(h[a][kv], scale[a][kv], x);
+      store_row<T, E>(static_cast<T*>(kv ? p.v : p.k) + (unit0 + a * kRows + sub) * DIM + feature, x);
+    }
   }
 }
 

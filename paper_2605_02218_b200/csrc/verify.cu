@@ -45,6 +45,8 @@ int check_cache(const covspec_cache* c) {
   const long long least = (long long)c->heads * c->page_size * c->head_dim;
   if (c->k_page_stride < least || c->v_page_stride < least) return COVSPEC_ERR_SHAPE;
   const int e = bytes_of(c->store);
+  // the kernels count rows of a cache in 16 bytes
+  if (std::max(c->k_page_stride, c->v_page_stride) > (1ll << 36) / e / c->pages) return COVSPEC_ERR_UNSUPPORTED;
   if (c->k_page_stride * e % 16 || c->v_page_stride * e % 16 || !aligned16(c->k) || !aligned16(c->v)) return COVSPEC_ERR_ARG;
   return COVSPEC_OK;
 }
@@ -91,6 +93,12 @@ int sm_count(int* sms) {
   return COVSPEC_OK;
 }
 
+// CTAs of the cache kernels for `rows` (token, head) rows of `lanes` lanes each.
+long long cache_grid(long long rows, int lanes) {
+  const long long per = (long long)(32 / lanes) * cache::kPasses * (cache::kThreads / 32);
+  return (rows + per - 1) / per;
+}
+
 // Largest request, as rows of a key head, that the attention kernel for few rows takes when both run; its CTAs: two per SM.
 constexpr int kFewRows = 64, kRowsCtas = 2;
 long long part_bytes(int ctas, int rows, int dim) { return 2ll * ctas * rows * (dim + 2) * 4; }
@@ -134,7 +142,7 @@ int covspec_cache_write(const covspec_cache* cache, const covspec_tokens* tokens
   if (!k || !v || !aligned16(k) || !aligned16(v)) return COVSPEC_ERR_ARG;
   if (k_stride < width || v_stride < width) return COVSPEC_ERR_SHAPE;
   if (k_stride * bytes_of(dtype) % 16 || v_stride * bytes_of(dtype) % 16) return COVSPEC_ERR_ARG;
-  const long long grid = ((long long)n * cache->heads * (cache->head_dim / 8) + cache::kThreads - 1) / cache::kThreads;
+  const long long grid = cache_grid((long long)n * cache->heads, cache->head_dim / 8);
   if (grid > INT_MAX) return COVSPEC_ERR_SHAPE;
   cache::WriteParams prm{pages_of(cache), tokens_of(tokens), k, v, k_stride, v_stride, n, rows, row_offsets, source_rows};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
@@ -158,7 +166,7 @@ int covspec_cache_read(const covspec_cache* cache, const covspec_tokens* tokens,
   if (n < 0) return COVSPEC_ERR_SHAPE;
   if (n == 0) return COVSPEC_OK;
   if (!k || !v || !aligned16(k) || !aligned16(v)) return COVSPEC_ERR_ARG;
-  const long long grid = ((long long)n * cache->heads * (cache->head_dim / 8) + cache::kThreads - 1) / cache::kThreads;
+  const long long grid = cache_grid((long long)n * cache->heads, cache->head_dim * bytes_of(cache->store) / 16);
   if (grid > INT_MAX) return COVSPEC_ERR_SHAPE;
   cache::ReadParams prm{pages_of(cache), tokens_of(tokens), k, v, n};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
@@ -274,17 +282,23 @@ int covspec_edit_logits(int logit_dtype, int rows, int vocab, long long ld, cons
   prm.mask = static_cast<const unsigned char*>(e.mask); prm.mask_ld = e.mask_stride;
   int sms = 0;
   if (const int st = sm_count(&sms)) return st;
+  // Rows of a CTA share the tables of their request, which cost a pass over the history; segments of 4096 entries and groups of
+  // rows as long as two CTAs an SM are left, then smaller ones (8 rows x 151674: see the design notes).
   prm.segment = 4096;
   prm.group = 1;
-  const unsigned segments = (unsigned)((vocab + prm.segment - 1) / prm.segment);
-  while (prm.group < 16 && (long long)segments * ((rows + 2 * prm.group - 1) / (2 * prm.group)) >= 4ll * sms) prm.group *= 2;
+  auto segments_of = [&] { return (unsigned)((vocab + prm.segment - 1) / prm.segment); };
+  while (prm.group < 16 && prm.group < rows && (long long)segments_of() * ((rows + 2 * prm.group - 1) / (2 * prm.group)) >= 4ll * sms) prm.group *= 2;
+  while (prm.segment > 2048 && (long long)segments_of() * rows < 2ll * sms) prm.segment /= 2;
+  while ((rows + prm.group - 1) / prm.group > 65535) prm.group *= 2;
+  const unsigned segments = segments_of();
   const int groups = (rows + prm.group - 1) / prm.group;
-  if (groups > 65535) return COVSPEC_ERR_SHAPE;
-  const size_t smem = (size_t)prm.segment * (e.bias_ids ? 8 : 4);
+  const int smem = prm.segment / 8 + prm.segment * (e.bias_ids ? 8 : 4);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   CUDA_TRY(with_type(logit_dtype, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
-    edit::edit_kernel<T><<<dim3(segments, (unsigned)groups), edit::kThreads, smem, s>>>(prm);
+    const cudaError_t err = allow_shared<edit::edit_kernel<T>>(4096 / 8 + 4096 * 8);
+    if (err != cudaSuccess) return err;
+    edit::edit_kernel<T><<<dim3(segments, (unsigned)groups), edit::kThreads, (size_t)smem, s>>>(prm);
     return cudaGetLastError();
   }));
   return COVSPEC_OK;
