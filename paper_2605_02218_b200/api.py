@@ -174,8 +174,8 @@ _native = None
 
 
 def _load_native(lib, path: str):
-    """The native part of the binding with the library's functions given to it, or None: the three calls that it makes
-    shorter then go through ctypes."""
+    """The native part of the binding with the library's functions given to it, or None: the calls that it makes shorter then
+    go through ctypes."""
     if not os.path.exists(path):
         return None
     try:
@@ -187,7 +187,8 @@ def _load_native(lib, path: str):
                       f"`python -m paper_2605_02218_b200.build`): {e}", RuntimeWarning)
         return None
     module.bind(*(C.cast(f, C.c_void_p).value for f in
-                  (lib.covspec_correct, lib.covspec_branch_candidates_host, lib.covspec_query_score_static)))
+                  (lib.covspec_correct, lib.covspec_branch_candidates_host, lib.covspec_query_score_static, lib.covspec_cache_write,
+                   lib.covspec_cache_read, lib.covspec_cache_attend, lib.covspec_edit_logits)))
     return module
 
 
@@ -645,12 +646,13 @@ class PagedCache:
             raise ValueError("k_scale, v_scale: required of the 8-bit types and of no other")
         pages, heads, page_size, head_dim = k.shape
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._held = (k, v, k_scale, v_scale)      # the addresses below are theirs
         self._c = Cache(store, _c_int(pages, "pages"), _c_int(heads, "heads"), _c_int(page_size, "page_size"), head_dim,
                         k.data_ptr(), v.data_ptr(),
                         *(_addr(s, n, torch.float32, k.device, pages * heads * page_size)
                           for n, s in (("k_scale", k_scale), ("v_scale", v_scale))),
                         *(t.stride(0) if pages > 1 else page for t in (k, v)))
-        self._ref = C.byref(self._c)
+        self._ref, self._at, self._work = C.byref(self._c), C.addressof(self._c), {}
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, dtype: torch.dtype, device="cuda") -> "PagedCache":
@@ -684,6 +686,14 @@ class PagedCache:
         one projection) into the cache.  With `rows` and `row_offsets` token i of request b is row row_offsets[b] + rows[i]:
         Pruner.select's keep_idx and the visual offsets (int32, on the device) write the kept tokens of a prefill."""
         lib, dev = _lib or load_library(), self.k.device
+        st = None if _native is None else _native.cache_write(self._at, self.k, k, v, offsets, lengths, table, rows, row_offsets)
+        if st is None:
+            st = self._write(lib, dev, k, v, offsets, lengths, table, rows, row_offsets)
+        if st:
+            raise CovspecError(st, "covspec_cache_write")
+
+    def _write(self, lib, dev, k, v, offsets, lengths, table, rows, row_offsets) -> int:
+        """The call for arguments of every kind that the library can take; says what is wrong with others."""
         dtype = k.dtype if isinstance(k, torch.Tensor) else None
         if dtype not in _LOGIT_DTYPES:
             raise TypeError(f"k: float32, bfloat16 or float16 is required, not {dtype}")
@@ -698,15 +708,19 @@ class PagedCache:
         n = k.shape[0] if rows is None else rows.numel()
         rp, rop = _addr(rows, "rows", torch.int32, dev, n), _addr(row_offsets, "row_offsets", torch.int32, dev, tokens.batch + 1)
         with torch.cuda.device(dev):
-            st = lib.covspec_cache_write(self._ref, C.byref(tokens), _LOGIT_DTYPES[dtype], _c_int(n, "tokens"), kp, vp, ks, vs, rp, rop,
-                                         _c_int(k.shape[0], "rows of k"), _stream())
-        if st:
-            raise CovspecError(st, "covspec_cache_write")
+            return lib.covspec_cache_write(self._ref, C.byref(tokens), _LOGIT_DTYPES[dtype], _c_int(n, "tokens"), kp, vp, ks, vs, rp, rop,
+                                           _c_int(k.shape[0], "rows of k"), _stream())
 
     def read(self, offsets: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, n: int, dtype: torch.dtype = torch.bfloat16):
         """covspec_cache_read: (k, v), [n, heads, head_dim] each, of the `n` tokens that `offsets` delimits; rows of no request
         are undefined."""
         lib, dev = _lib or load_library(), self.k.device
+        if _native is not None and dtype in _LOGIT_DTYPES:
+            got = _native.cache_read(self._at, self.k, offsets, lengths, table, n, _LOGIT_DTYPES[dtype])
+            if type(got) is tuple:
+                return got
+            if got is not None:
+                raise CovspecError(got, "covspec_cache_read")
         tokens = self._tokens(offsets, lengths, table)
         if dtype not in _LOGIT_DTYPES:
             raise TypeError(f"dtype: float32, bfloat16 or float16 is required, not {dtype}")
@@ -729,6 +743,26 @@ class PagedCache:
         lib, dev = _lib or load_library(), self.k.device
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("q: [tokens, q_heads, head_dim] is required")
+        if scale is None:
+            scale = self._c.head_dim ** -0.5
+        heads = q.shape[1]
+        size = self._work.get(heads)
+        if size is None:
+            with torch.cuda.device(dev):
+                size = lib.covspec_cache_attend_workspace(self._ref, _c_int(heads, "q_heads"))
+            if size < 0:
+                raise CovspecError(int(size), "covspec_cache_attend")
+            self._work[heads] = size
+        if _native is not None:
+            got = _native.cache_attend(self._at, self.k, size, q, offsets, lengths, table, scale, window, max_new, lse, out)
+            if got is not None:
+                if type(got) is int:
+                    raise CovspecError(got, "covspec_cache_attend")
+                return got
+        return self._attend(lib, dev, size, q, offsets, lengths, table, scale, window, max_new, lse, out)
+
+    def _attend(self, lib, dev, size, q, offsets, lengths, table, scale, window, max_new, lse, out):
+        """The call for arguments of every kind that the library can take; says what is wrong with others."""
         dtype = q.dtype
         if dtype not in (torch.bfloat16, torch.float16):
             raise TypeError(f"q: bfloat16 or float16 is required, not {dtype}")
@@ -742,13 +776,10 @@ class PagedCache:
             raise ValueError(f"out: {out.shape[0]} rows, {n} are written")
         logs = torch.empty(n, heads, dtype=torch.float32, device=dev) if lse else None
         with torch.cuda.device(dev):
-            size = lib.covspec_cache_attend_workspace(self._ref, _c_int(heads, "q_heads"))
-            if size < 0:
-                raise CovspecError(int(size), "covspec_cache_attend")
             # from torch's pool, like the outputs: it knows streams and captures, so no two calls in flight share it
             work = torch.empty(size, dtype=torch.uint8, device=dev)
             st = lib.covspec_cache_attend(self._ref, C.byref(tokens), _LOGIT_DTYPES[dtype], _c_int(n, "tokens"), qp, qs, heads,
-                                          float(scale) if scale is not None else self._c.head_dim ** -0.5, _c_int(window, "window"),
+                                          float(scale), _c_int(window, "window"),
                                           _c_int(max_new, "max_new"), op, os_, _ptr(logs), work.data_ptr(), size, _stream())
         if st:
             raise CovspecError(st, "covspec_cache_attend")
@@ -768,6 +799,13 @@ def edit_logits(z: torch.Tensor, row_offsets: torch.Tensor, *, history: Optional
     word w / 32 allows token w.  Everything on z's device, ids and offsets int32, factors float32.  Returns the edited logits (in
     `out` if given, which may be z); rows of no request and columns past the vocabulary are undefined, or left as they were."""
     lib = _lib or load_library()
+    if _native is not None:
+        got = _native.edit_logits(z, row_offsets, history, history_offsets, prompt_lengths, drafted, repetition, presence, frequency,
+                                  bias_ids, bias_values, bias_offsets, mask, vocab, out)
+        if got is not None:
+            if type(got) is int:
+                raise CovspecError(got, "covspec_edit_logits")
+            return got
     if not isinstance(z, torch.Tensor) or z.dim() != 2 or z.dtype not in _LOGIT_DTYPES:
         raise TypeError("z: a matrix of float32, bfloat16 or float16 is required")
     if not z.is_cuda:

@@ -103,7 +103,7 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
 def build_binding(force: bool = False) -> str:
     import torch
     target = binding_path()
-    if not force and os.path.exists(target) and os.path.getmtime(BINDING_SOURCE) <= os.path.getmtime(target):
+    if not force and os.path.exists(target) and _newest(_files_of(BINDING_SOURCE)) <= os.path.getmtime(target):
         return target
     base = os.path.dirname(torch.__file__)
     libs = os.path.join(base, "lib")
@@ -111,7 +111,7 @@ def build_binding(force: bool = False) -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-shared", "-fPIC", "-std=c++17",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-I", os.path.join(base, "include"), "-I", os.path.join(base, "include", "torch", "csrc", "api", "include"),
-           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"),
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"),
            "-o", target, BINDING_SOURCE, "-L", libs, "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python",
            "-Wl,-rpath," + libs]
     res = subprocess.run(cmd, capture_output=True, text=True)

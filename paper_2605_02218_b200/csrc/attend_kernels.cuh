@@ -1,29 +1,34 @@
 // Attention of few rows per key head (single tokens, drafted blocks) over the paged cache: one pass over the keys with running
-// maxima and sums.  A tile is 16, 32 or 64 rows (16 a warp; warps left over share the keys of a unit) and 64 keys.  The work is
+// maxima and sums.  A tile is 16, 32 or 64 rows (16 a warp; warps left over share the keys of a unit) and 64 keys, with 8-bit rows and 16-row tiles 128.  The work is
 // bound by reading the cache, so operands go to the tensor cores through registers (mma.sync): shared memory holds the pages'
 // rows as they are in the cache, 8-bit ones are widened in registers.
 //
-// 8-bit rows are exact in 16 bits, so their scales stay outside the products: s_ij = (q_i . k_j) * key scale, and the probability
+// 8-bit rows are exact in float16, so their scales stay outside the products: s_ij = (q_i . k_j) * key scale, and the probability
 // takes the value's scale before it is rounded to 16 bits.  So that it cannot leave float16's range, the running maximum is the
-// one of s_ij + log2(value scale).
+// one of s_ij + the exponent of the value's scale.
 #pragma once
+#include <type_traits>
+
 #include "attend_common.cuh"
 
 namespace covspec {
 namespace attend {
 
-constexpr int kKeys = 64;
 constexpr int kThreads = 128;
 
-template <int STORE, int DIM> struct Layout {
-  static constexpr int kBytes = STORE >= cache::kE4M3 ? 1 : 2;
-  static constexpr int kRow = DIM * kBytes;                    // bytes of a key's row
+template <int STORE, int DIM, int ROWS> struct Layout {
+  static constexpr bool k8 = STORE >= cache::kE4M3;
+  static constexpr int kKeys = k8 && ROWS == 16 ? 128 : 64;    // of a unit
+  static constexpr int kCtas = 2;                              // on an SM
+  static constexpr int kRow = DIM * (k8 ? 1 : 2);              // bytes of a key's row
   static constexpr int kChunks = kRow / 16;
   static constexpr int kStage = 2 * kKeys * kRow;              // keys, values
-  static constexpr int kStages = kStage >= 32768 ? 3 : 6;
-  static constexpr int kScale = STORE >= cache::kE4M3 ? 2 * kKeys * 4 : 0;   // per stage: the keys' and the values' scales
-  static constexpr int kSmem = kStages * (kStage + kScale) + 2 * 2 * kKeys * 4   // places of two units
-                               + (kStages + 1) * 8 + 2 * 16 * 8 + 128;           // keys there; maxima and sums of two warps' rows
+  static constexpr int kScale = k8 ? 2 * kKeys * 4 : 0;        // per stage: the keys' and the values' scales
+  static constexpr int kFixed = 2 * 2 * kKeys * 4 + 8 * 16 + 2 * 16 * 8 + 128;   // places of two units; keys there; maxima and sums of two warps' rows
+  static constexpr int kFit = (233472 / kCtas - 1024 - 128 - kFixed) / (kStage + kScale);   // an SM's shared memory, 1 KB of it a CTA's own
+  static constexpr int kStages = kFit < 6 ? kFit : 6;
+  static constexpr int kSmem = kStages * (kStage + kScale) + kFixed;
+  static_assert(kStages >= 2 && (ROWS == 64 || kStage >= 2 * 16 * DIM * 4));
 };
 // Byte offset of a 16-byte chunk of a row: chunks are permuted so that eight rows' chunks of one column lie in different banks.
 template <int ROW> __device__ __forceinline__ int swizzled(int row, int chunk) {
@@ -68,42 +73,50 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Two 8-bit values as two 16-bit ones; `sel` picks their bytes (prmt selector of the low and the high value).  Exact.
-//  e4m3: sign and the seven other bits are moved to where the wider type has them, which is the value over 2^120 (bf16) or 2^8
-//        (f16); the product with that power is exact, subnormal codes included.  The code of NaN does not occur in a cache.
-//  int8: the byte becomes the mantissa of a number with a known exponent, which is then taken off.
-template <typename T, int STORE>
-__device__ __forceinline__ uint32_t widen(uint32_t bytes, uint32_t sel) {
+// Two 8-bit values (bytes `lo` and `hi` of a word) as two float16, exactly.  8-bit keys and values are multiplied in float16
+// whatever the type of the queries: both widen to it in fewer instructions than to bfloat16 (four a pair), and probabilities
+// keep three more bits.  Queries in bfloat16 are brought to float16 by a power of two for each row (to_half).
+//  e4m3: the conversion instruction runs at about 8 values a cycle on an SM, so most pairs (!CVT) move their seven lower bits to
+//        where float16 has them, which is the value over 2^8, and multiply by that power, which is exact, subnormal codes
+//        included.  The code of NaN does not occur in a cache.
+//  int8: the byte becomes the lower bits of 1024 + (v + 128), and 1152 is taken off.
+template <int STORE, bool CVT>
+__device__ __forceinline__ uint32_t widen(uint32_t bytes, int lo, int hi) {
   uint32_t r;
-  if constexpr (STORE == cache::kE4M3) {
-    const uint32_t w = __byte_perm(bytes, 0u, sel);            // each value in the upper byte of its half, zeros below
-    if constexpr (__is_same(T, __half)) {
-      const uint32_t m = (w & 0x80008000u) | ((w & 0x7f007f00u) >> 1);
-      asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(0x5c005c00u));              // 2^8
-    } else {
-      const uint32_t m = (w & 0x80008000u) | ((w & 0x7f007f00u) >> 4);
-      asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(0x7b807b80u));             // 2^120
-    }
+  if constexpr (STORE == cache::kE4M3 && CVT) {
+    const uint32_t two = lo + 1 == hi && lo == 0 ? bytes : __byte_perm(bytes, 0u, (uint32_t)(lo | hi << 4));
+    asm("{\n.reg .b16 h;\ncvt.u16.u32 h, %1;\ncvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(r) : "r"(two));
+  } else if constexpr (STORE == cache::kE4M3) {
+    const uint32_t w = __byte_perm(bytes, 0u, (uint32_t)(4 | lo << 4 | 4 << 8 | hi << 12));   // in the halves' upper bytes
+    const uint32_t m = (w & 0x80008000u) | ((w >> 1) & 0x3f803f80u);
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(0x5c005c00u));
   } else {
-    if constexpr (__is_same(T, __half)) {
-      const uint32_t w = __byte_perm(bytes ^ 0x80808080u, 0x64646464u, sel);             // 1024 + (v + 128)
-      asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x64806480u));              // - 1152
-    } else {
-      const uint32_t w = __byte_perm(bytes, 0x43434343u, sel);                           // 128 + the lower seven bits ...
-      asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w & 0xff7fff7fu), "r"(w & 0xff80ff80u));   // ... - 128, or 256 for v < 0
-    }
+    const uint32_t w = __byte_perm(bytes ^ 0x80808080u, 0x64646464u, (uint32_t)(lo | 4 << 4 | hi << 8 | 4 << 12));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x64806480u));
   }
   return r;
 }
-// Selectors for the bytes (lo, hi): e4m3 wants them in the upper bytes of the halves, int8 in the lower ones.
-template <int STORE> __device__ constexpr uint32_t pick(int lo, int hi) {
-  return STORE == cache::kE4M3 ? (uint32_t)(4 | lo << 4 | 4 << 8 | hi << 12) : (uint32_t)(lo | 4 << 4 | hi << 8 | 4 << 12);
+// The power of two that brings numbers of at most `top` below 2^15 (1 for zero and for what is not finite), and its inverse.
+__device__ __forceinline__ float power_for(float top) {
+  const int e = (int)(__float_as_uint(top) >> 23);
+  return e == 0 || e == 255 ? 1.f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 253) << 23);
+}
+__device__ __forceinline__ float inverse_power(float f) { return __uint_as_float((254u << 23) - __float_as_uint(f)); }
+// Two bfloat16 as two float16, times f: exact but for numbers 2^-29 times as small as the row's largest.
+__device__ __forceinline__ uint32_t to_half(uint32_t two, float f) {
+  const __half2 h = __floats2half2_rn(__uint_as_float(two << 16) * f, __uint_as_float(two & 0xffff0000u) * f);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float largest_of(uint32_t two, float top) {
+  return fmaxf(top, fmaxf(fabsf(__uint_as_float(two << 16)), fabsf(__uint_as_float(two & 0xffff0000u))));
 }
 
 template <typename T, int STORE, int DIM, int ROWS>
-__global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
-  using L = Layout<STORE, DIM>;
-  constexpr bool k8 = STORE >= cache::kE4M3;
+__global__ void __launch_bounds__(kThreads, (Layout<STORE, DIM, ROWS>::kCtas)) attend_kernel(Params p) {
+  using L = Layout<STORE, DIM, ROWS>;
+  constexpr bool k8 = L::k8;
+  using M = std::conditional_t<k8, __half, T>;                 // type of the products
+  constexpr int kKeys = L::kKeys, kWords = kKeys / 32;
   constexpr int kWarpsM = ROWS / 16, kWarpsK = 4 / kWarpsM;    // warps along the rows, along the keys of a unit
   constexpr int kMine = kKeys / kWarpsK;                       // keys of a unit that one warp takes
   constexpr int kS = L::kStages;
@@ -112,7 +125,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
   float* scales = reinterpret_cast<float*>(smem + kS * L::kStage);
   uint32_t* places = reinterpret_cast<uint32_t*>(scales + kS * (L::kScale / 4));   // [2][2][kKeys]: keys', values' rows in 16 bytes
   float2* box_ts = reinterpret_cast<float2*>(places + 4 * kKeys);                  // [2][16]
-  uint32_t* there = reinterpret_cast<uint32_t*>(box_ts + 2 * 16);                  // [kS + 1][2]: which keys of a unit are there
+  uint32_t* there = reinterpret_cast<uint32_t*>(box_ts + 2 * 16);                  // [kS + 1][kWords]: which keys of a unit are there
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   const int wm = warp / kWarpsK, wk = warp % kWarpsK;
   const int g = lane >> 2, tq = lane & 3;
@@ -145,11 +158,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
       const bool ok = (unsigned)page < (unsigned)p.c.pages;
       const int in = (load.h << p.c.page_shift) + ((load.key + tid) & ((1 << p.c.page_shift) - 1));
       uint32_t* place = places + (issued & 1) * 2 * kKeys + tid;
-      auto row = [&](long long page_ld) { return (uint32_t)((unsigned long long)(page * page_ld + (long long)in * DIM) / (16 / L::kBytes)); };
+      auto row = [&](long long page_ld) { return (uint32_t)((unsigned long long)(page * page_ld + (long long)in * DIM) / (16 / (L::kRow / DIM))); };
       place[0] = ok ? row(p.c.k_page) : kNowhere;
       place[kKeys] = ok ? row(p.c.v_page) : kNowhere;
       const uint32_t bits = __ballot_sync(0xffffffffu, ok);
-      if (lane == 0) there[2 * word + warp] = bits;
+      if (lane == 0) there[kWords * word + warp] = bits;
       if constexpr (k8) scale_at = ok ? (((long long)page * p.c.heads) << p.c.page_shift) + in : -1;
     }
     word = word == kS ? 0 : word + 1;
@@ -196,6 +209,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
   uint32_t qf[DIM / 16][4];
   float o[DIM / 8][4], top[2], sum[2];
   int pos[2];                     // position of the thread's two rows; -1 where there is no row
+  [[maybe_unused]] float row_scale[2] = {p.scale_log2, p.scale_log2};
   int low = 0, high = 0;          // the lowest of them, the highest before the highest one's window
   int began = 0;                  // the item's first unit, counted from the share's
   bool fresh = true;
@@ -224,6 +238,17 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
           qf[s][i] = ok ? w[k8 ? 2 * tq : tq] : 0u;
           qf[s][2 + i] = ok ? w[k8 ? 2 * tq + 1 : tq + 4] : 0u;
         }
+        if constexpr (!__is_same(M, T)) {
+          float most = 0.f;
+#pragma unroll
+          for (int s = 0; s < DIM / 16; ++s) most = largest_of(qf[s][2 + i], largest_of(qf[s][i], most));
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+          const float f = power_for(most);
+#pragma unroll
+          for (int s = 0; s < DIM / 16; ++s) { qf[s][i] = to_half(qf[s][i], f); qf[s][2 + i] = to_half(qf[s][2 + i], f); }
+          row_scale[i] = p.scale_log2 * inverse_power(f);
+        }
         top[i] = -INFINITY;
         sum[i] = 0.f;
       }
@@ -248,18 +273,21 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
         ldm4(kf, tc::smem_u32(kbase + swizzled<L::kRow>(row, c + (lane >> 3))));
         if constexpr (k8) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            mma<T>(s[j], qf[c + i], widen<T, STORE>(kf[i], pick<STORE>(0, 1)), widen<T, STORE>(kf[i], pick<STORE>(2, 3)));
+          for (int i = 0; i < 4; i += 2) {                      // every other chunk by conversions: both units are kept busy
+            mma<M>(s[j], qf[c + i], widen<STORE, true>(kf[i], 0, 1), widen<STORE, true>(kf[i], 2, 3));
+            mma<M>(s[j], qf[c + i + 1], widen<STORE, false>(kf[i + 1], 0, 1), widen<STORE, false>(kf[i + 1], 2, 3));
+          }
         } else {
-          mma<T>(s[j], qf[c / 2], kf[0], kf[1]);
-          mma<T>(s[j], qf[c / 2 + 1], kf[2], kf[3]);
+          mma<M>(s[j], qf[c / 2], kf[0], kf[1]);
+          mma<M>(s[j], qf[c / 2 + 1], kf[2], kf[3]);
         }
       }
     }
     // ---- running maxima and sums ----
     const float* sc = scales + stage * 2 * kKeys + wk * kMine;
-    uint64_t see_all = (uint64_t)there[2 * seen + 1] << 32 | there[2 * seen];
-    see_all >>= wk * kMine;
+    uint64_t see_all;                                          // of this warp's keys
+    if constexpr (kMine == 64) see_all = (uint64_t)there[kWords * seen + 1] << 32 | there[kWords * seen];
+    else see_all = there[kWords * seen + wk * kMine / 32] >> (wk * kMine % 32);
     const int key0 = at.key + wk * kMine;
     // every row of the warp sees all of its keys
     const bool clear = (kMine == 64 ? see_all == ~0ull : (see_all & ((1ull << (kMine & 63)) - 1)) == (1ull << (kMine & 63)) - 1) &&
@@ -267,19 +295,18 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
     float best[2] = {top[0], top[1]};
 #pragma unroll
     for (int j = 0; j < kMine / 8; ++j) {
-      float by[2] = {p.scale_log2, p.scale_log2};
-      [[maybe_unused]] float lift[2] = {0.f, 0.f};
+      [[maybe_unused]] float by[2], lift[2];
       if constexpr (k8) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          by[i] *= sc[j * 8 + 2 * tq + i];
+          by[i] = sc[j * 8 + 2 * tq + i];
           lift[i] = exponent_of(sc[kKeys + j * 8 + 2 * tq + i]);
         }
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int col = j * 8 + 2 * tq + (e & 1), i = e >> 1;
-        s[j][e] *= by[e & 1];
+        s[j][e] *= k8 ? by[e & 1] * row_scale[i] : p.scale_log2;
         if (!clear) {
           const int key = key0 + col;
           const bool see = (see_all >> col) & 1u && key <= pos[i] && (p.window == 0 || key > pos[i] - p.window);
@@ -312,8 +339,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
         sum[x >> 1] += e[x];
         if constexpr (k8) e[x] *= sc[kKeys + j * 8 + 2 * tq + (x & 1)];
       }
-      pf[j / 2][(j & 1) * 2] = pack2of<T>(e[0], e[1]);
-      pf[j / 2][(j & 1) * 2 + 1] = pack2of<T>(e[2], e[3]);
+      pf[j / 2][(j & 1) * 2] = pack2of<M>(e[0], e[1]);
+      pf[j / 2][(j & 1) * 2 + 1] = pack2of<M>(e[2], e[3]);
     }
     // ---- values ----
 #pragma unroll
@@ -327,8 +354,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             // a register holds features 2n, 2n + 1 of two keys: the even ones make one tile of eight columns, the odd ones another
-            mma<T>(o[2 * (c + h)], pf[s16], widen<T, STORE>(vf[2 * h], pick<STORE>(0, 2)), widen<T, STORE>(vf[2 * h + 1], pick<STORE>(0, 2)));
-            mma<T>(o[2 * (c + h) + 1], pf[s16], widen<T, STORE>(vf[2 * h], pick<STORE>(1, 3)), widen<T, STORE>(vf[2 * h + 1], pick<STORE>(1, 3)));
+            mma<M>(o[2 * (c + h)], pf[s16], widen<STORE, false>(vf[2 * h], 0, 2), widen<STORE, false>(vf[2 * h + 1], 0, 2));
+            mma<M>(o[2 * (c + h) + 1], pf[s16], widen<STORE, false>(vf[2 * h], 1, 3), widen<STORE, false>(vf[2 * h + 1], 1, 3));
           }
         }
       } else {
@@ -336,8 +363,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(Params p) {
         for (int c = 0; c < L::kChunks; c += 2) {
           uint32_t vf[4];
           ldm4t(vf, tc::smem_u32(vbase + swizzled<L::kRow>(row0 + (lane & 15), c + (lane >> 4))));
-          mma<T>(o[c], pf[s16], vf[0], vf[1]);
-          mma<T>(o[c + 1], pf[s16], vf[2], vf[3]);
+          mma<M>(o[c], pf[s16], vf[0], vf[1]);
+          mma<M>(o[c + 1], pf[s16], vf[2], vf[3]);
         }
       }
     }

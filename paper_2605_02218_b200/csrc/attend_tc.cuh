@@ -35,7 +35,7 @@ template <int STORE, int DIM> struct Layout {
   static constexpr int kQ = kRows * DIM * 2;
   static constexpr int kSlots = k8 ? 4 : 5;
   static constexpr int kTail = 4 * 16                          // which keys of a unit are there, 4 units
-                               + (k8 ? 4 * 2 * kKeys * 4 : 0)  // scales of 4 units
+                               + (k8 ? 4 * 2 * kKeys * 4 + 2 * kRows * 4 : 0)   // scales of 4 units; of the query rows of 2 items
                                + 2 * kKeys * 8                 // places of a unit's keys, 2 units
                                + 256;                          // barriers, TMEM base, scratch
   static constexpr int kUsed = kQ + kSlots * kSlot + kTail;
@@ -123,14 +123,17 @@ template <typename T, int STORE, int DIM>
 __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
   using L = Layout<STORE, DIM>;
   constexpr bool k8 = L::k8;
+  using M = std::conditional_t<k8, __half, T>;                 // type of the products
+  constexpr bool kConvert = !__is_same(M, T);                  // queries to float16
   constexpr int kSlots = L::kSlots;
   extern __shared__ __align__(1024) uint8_t wide_smem[];
   uint8_t* smem = wide_smem;
   uint8_t* ring = smem + L::kQ;
   uint8_t* tail = ring + kSlots * L::kSlot;
   uint32_t* there = reinterpret_cast<uint32_t*>(tail);                       // [4][4]
-  float* scales = reinterpret_cast<float*>(tail + 64);                       // [4][2][kKeys]: key scale * scale_log2, value scale
-  uint32_t* places = reinterpret_cast<uint32_t*>(tail + 64 + (k8 ? 4 * 2 * kKeys * 4 : 0));  // [2][2][kKeys]: keys', values' rows in 16 bytes
+  float* scales = reinterpret_cast<float*>(tail + 64);                       // [4][2][kKeys]: key scale, value scale
+  float* row_scales = scales + 4 * 2 * kKeys;                                // [2][kRows]
+  uint32_t* places = reinterpret_cast<uint32_t*>(tail + 64 + (k8 ? 4 * 2 * kKeys * 4 + 2 * kRows * 4 : 0));  // [2][2][kKeys]: keys', values' rows in 16 bytes
   uint64_t* bars = reinterpret_cast<uint64_t*>(places + 4 * kKeys);
   uint64_t *full = bars, *empty = bars + 5, *q_full = bars + 10, *q_empty = bars + 11, *s_full = bars + 12, *p_ready = bars + 14,
            *o_full = bars + 16, *drained = bars + 18;                        // 19 barriers
@@ -192,6 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
     int slot = 0;
     uint32_t phase = 1, q_phase = 1;
     bool ok = true, fresh = true;
+    [[maybe_unused]] int items = 0;
     auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
     int page[2] = {-1, -1};
     auto look_up = [&] {                                       // pages of this thread's keys of the unit at `at`
@@ -213,13 +217,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         constexpr int kChunks = DIM / 8, kAtOnce = 32 / kChunks;
         const int chunk = lane % kChunks;
 #pragma unroll 4
-        for (int row = wp * kAtOnce + lane / kChunks; row < kRows; row += 3 * kAtOnce) {
-          const int r = at.tile * kRows + row;
-          const bool there_is = ok && r < at.r.rows;
-          const T* q = static_cast<const T*>(p.q) +
-                       (there_is ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM + chunk * 8 : 0);
-          copy16(smem_u32(smem + (row >> 7) * (128 * DIM * 2) + tile_at(128, row & 127, chunk)), q, there_is);
+        for (int row0 = wp * kAtOnce; row0 < kRows; row0 += 3 * kAtOnce) {
+          const int row = row0 + lane / kChunks, r = at.tile * kRows + row;
+          const bool in = row < kRows, is = ok && in && r < at.r.rows;
+          const T* q = static_cast<const T*>(p.q) + (is ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM + chunk * 8 : 0);
+          uint8_t* to = smem + (row >> 7) * (128 * DIM * 2) + tile_at(128, row & 127, chunk);
+          if constexpr (!kConvert) {
+            if (in) copy16(smem_u32(to), q, is);
+          } else {
+            uint4 w = is ? *reinterpret_cast<const uint4*>(q) : make_uint4(0u, 0u, 0u, 0u);
+            float most = largest_of(w.x, largest_of(w.y, largest_of(w.z, largest_of(w.w, 0.f))));
+#pragma unroll
+            for (int o = kChunks / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            const float f = power_for(most);
+            if (in) {
+              *reinterpret_cast<uint4*>(to) = make_uint4(to_half(w.x, f), to_half(w.y, f), to_half(w.z, f), to_half(w.w, f));
+              if (chunk == 0) row_scales[items * kRows + row] = inverse_power(f);
+            }
+          }
         }
+        items ^= 1;
         close(q_full);
       }
       // places of the unit's keys: a thread has key t, the first warp the last 32 too; the pages of the next unit's keys are under
@@ -237,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
           if constexpr (k8) {
             const long long w = (((long long)page[i] * p.c.heads) << p.c.page_shift) + row;
             if (is[i]) {
-              ks[i] = p.c.k_scale[w] * p.scale_log2;
+              ks[i] = p.c.k_scale[w];
               vs[i] = p.c.v_scale[w];
             }
           }
@@ -299,8 +316,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
             uint32_t v[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              v[2 * e] = widen<T, STORE>(w[e], pick<STORE>(0, 1));
-              v[2 * e + 1] = widen<T, STORE>(w[e], pick<STORE>(2, 3));
+              v[2 * e] = widen<STORE, true>(w[e], 0, 1);
+              v[2 * e + 1] = widen<STORE, false>(w[e], 2, 3);
             }
             *reinterpret_cast<uint4*>(dst + tile_at(kKeys, row, 2 * chunk)) = make_uint4(v[0], v[1], v[2], v[3]);
             *reinterpret_cast<uint4*>(dst + tile_at(kKeys, row, 2 * chunk + 1)) = make_uint4(v[4], v[5], v[6], v[7]);
@@ -314,7 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
     flush();
   } else if (warp == 11) {
     // ---------------- products ----------------
-    const uint32_t qk = idesc<T>(kKeys, false), pv = idesc<T>(DIM, true);
+    const uint32_t qk = idesc<M>(kKeys, false), pv = idesc<M>(DIM, true);
     int k_slot = 0, slot = 0;                                  // slot of the keys in S, next slot of the ring
     uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0};
     bool ok = true;
@@ -402,7 +419,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
     // ---------------- softmax ----------------
     const int x = warp >> 2, row = tid & 127;
     const uint32_t s_at = tmem + x * 128 + ((uint32_t)(warp & 3) << 21), o_at = s_at + kO;
-    float ref = 0.f, sum = 0.f;
+    float ref = 0.f, sum = 0.f, row_scale = 0.f;
+    int items = 1;                                             // items so far, the parity
+    bool unread = true;
     int pos = -1;
     int began = 0;                                             // the item's first unit, counted from the share's
     bool fresh = true, ok = true, active = false;
@@ -416,6 +435,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         const bool is = r < at.r.rows;
         pos = is ? at.r.length - at.r.n + r / p.group : -1;
         ref = is ? -INFINITY : 0.f;                            // rows past the end never ask for a reference
+        items ^= 1;
+        unread = true;
         sum = 0.f;
       }
       if (active) {
@@ -424,6 +445,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         tc_fence_after();
         const uint4 bits = *reinterpret_cast<const uint4*>(there + (u & 3) * 4);
         const float* sc = scales + (u & 3) * 2 * kKeys;
+        if (unread) {                                          // the item's first unit: its queries are there
+          row_scale = kConvert ? row_scales[items * kRows + x * 128 + row] * p.scale_log2 : p.scale_log2;
+          unread = false;
+        }
         // every row of the warp sees all keys of the unit
         const bool clear = (bits.x & bits.y & bits.z & bits.w) == 0xffffffffu &&
                            __all_sync(0xffffffffu, pos < 0 ? r >= at.r.rows : at.key + kKeys - 1 <= pos && (p.window == 0 || at.key > pos - p.window));
@@ -439,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         uint32_t packed[64];
         float more = 0.f, most = 0.f;                          // sums of the probabilities, without and with the values' scales
         auto make = [&](float safe, auto masked) {
-          const f32x2 low = pack2(-safe, -safe), by = pack2(p.scale_log2, p.scale_log2);
+          const f32x2 low = pack2(-safe, -safe), by = pack2(row_scale, row_scale);
           f32x2 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)}, most2 = pack2(0.f, 0.f);
           uint32_t v[2][16];
           tmem_fetch(s_at, v[0]);
@@ -456,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
               [[maybe_unused]] f32x2 g[2] = {by, by};
               if constexpr (k8) {
                 const float4 a = *reinterpret_cast<const float4*>(sc + 16 * c + e), b = *reinterpret_cast<const float4*>(sc + kKeys + 16 * c + e);
-                f[0] = pack2(a.x, a.y); f[1] = pack2(a.z, a.w);
+                f[0] = mul2(pack2(a.x, a.y), by); f[1] = mul2(pack2(a.z, a.w), by);
                 g[0] = pack2(b.x, b.y); g[1] = pack2(b.z, b.w);
               }
 #pragma unroll
@@ -475,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
                   most2 = add2(most2, t2);
                   t = unpack2(t2);
                 }
-                packed[8 * c + e / 2 + i] = pack2of<T>(t.x, t.y);
+                packed[8 * c + e / 2 + i] = pack2of<M>(t.x, t.y);
               }
             }
             if (c < 7) tmem_arrived(v[(c + 1) & 1]);
@@ -500,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const int key = 16 * c + e;
-              const float t = k8 ? v[e] * sc[key] + log2f(sc[kKeys + key]) : v[e] * p.scale_log2;
+              const float t = k8 ? v[e] * (sc[key] * row_scale) + log2f(sc[kKeys + key]) : v[e] * row_scale;
               best = (see >> e) & 1u ? fmaxf(best, t) : best;
             }
           }

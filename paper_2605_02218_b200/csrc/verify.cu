@@ -99,14 +99,14 @@ long long cache_grid(long long rows, int lanes) {
   return (rows + per - 1) / per;
 }
 
-// Largest request, as rows of a key head, that the attention kernel for few rows takes when both run; its CTAs: two per SM.
+// Largest request, as rows of a key head, that the attention kernel for few rows takes when both run; its CTAs at most per SM.
 constexpr int kFewRows = 64, kRowsCtas = 2;
 long long part_bytes(int ctas, int rows, int dim) { return 2ll * ctas * rows * (dim + 2) * 4; }
 
 template <typename T, int STORE, int DIM, int ROWS>
 cudaError_t launch_rows(const attend::Params& prm, int ctas, cudaStream_t s) {
   constexpr auto kernel = attend::attend_kernel<T, STORE, DIM, ROWS>;
-  constexpr int smem = attend::Layout<STORE, DIM>::kSmem;
+  constexpr int smem = attend::Layout<STORE, DIM, ROWS>::kSmem;
   cudaError_t e = allow_shared<kernel>(smem);
   if (e != cudaSuccess) return e;
   e = launch_dependent(kernel, dim3((unsigned)ctas), attend::kThreads, smem, s, prm);
@@ -234,7 +234,7 @@ int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* token
     const long long items = ((long long)n * prm.group / rows + prm.t.batch) * cache->heads;
     return (int)std::min<long long>(ctas, items * (((long long)prm.t.width * cache->page_size + keys - 1) / keys + 1));
   };
-  const int ctas = ctas_of(rows, attend::kKeys, kRowsCtas * sms);
+  const int ctas = ctas_of(rows, 64, kRowsCtas * sms);
   attend::Params wide = prm;
   wide.rows_over = kFewRows;
   wide.open = prm.open + 2ll * kRowsCtas * sms;
