@@ -237,7 +237,7 @@ int covspec_correct(int logit_dtype, int rows, int vocab, long long ld, const vo
 typedef struct {
   int store;
   int pages, heads;
-  int page_size;               /* positions in a page: a power of two, at most 4096                */
+  int page_size;               /* positions in a page: a power of two, 8 to 4096                   */
   int head_dim;                /* 64 or 128                                                        */
   void* k;
   void* v;

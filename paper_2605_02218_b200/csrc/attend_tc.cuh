@@ -5,9 +5,10 @@
 // tiles; the probabilities overwrite S in 16 bits and are the A operand of the second product from there.  Keys are K-major, values
 // MN-major (keys are the inner dimension of the second product), both as rows of 64 features in 128-byte swizzled tiles.
 //
-// Warps: 0-3 and 4-7 softmax of tile 0 and 1, a row a thread; 8-10 bring queries, keys and values into shared memory, 16-bit rows by
-// asynchronous copies, 8-bit ones through registers, where they are widened (attend_kernels.cuh); 11 issues the products.  Twelve
-// warps leave each thread 168 registers; with 16 and registers moved between them, some of either kind spilled.
+// Warps: 0-7 and 8-15 softmax of tile 0 and 1, a row of it two threads in two warps, each half of a unit's keys; 16 issues the
+// products; 17-19 bring queries, keys and values into shared memory.  16-bit keys and values come by tiled copies, a box as many rows
+// as a page has (at most 128), issued by one warp, a box a lane; where not every key of a unit is there, the values' other rows
+// are cleared before the products may see them.  8-bit ones come through registers, where they are widened (attend_kernels.cuh).
 //
 // The running maximum is only a reference that keeps the exponentials in range: a row keeps it
 // while a unit's probabilities add up to at most 2^14, so that O is rescaled seldom and one pass over S makes the probabilities.  A
@@ -24,8 +25,8 @@ namespace wide {
 using namespace tc;
 
 constexpr int kRows = 256, kKeys = 128;
-constexpr int kThreads = 12 * 32;
-constexpr int kProducers = 96;
+constexpr int kThreads = 20 * 32, kSoftmaxWarps = 16;
+constexpr int kCopyWarps = 3, kProducers = kCopyWarps * 32;
 constexpr float kMost = 16384.f;            // a unit's probabilities add up to no more over their reference
 
 template <int STORE, int DIM> struct Layout {
@@ -34,10 +35,10 @@ template <int STORE, int DIM> struct Layout {
   static constexpr int kRow = DIM * (k8 ? 1 : 2);              // bytes of a row in the cache
   static constexpr int kQ = kRows * DIM * 2;
   static constexpr int kSlots = k8 ? 4 : 5;
-  static constexpr int kTail = 4 * 16                          // which keys of a unit are there, 4 units
+  static constexpr int kTail = 4 * 16 + 4 * 32                 // which keys of a unit are there, its item; 4 units
                                + (k8 ? 4 * 2 * kKeys * 4 + 2 * kRows * 4 : 0)   // scales of 4 units; of the query rows of 2 items
-                               + 2 * kKeys * 8                 // places of a unit's keys, 2 units
-                               + 256;                          // barriers, TMEM base, scratch
+                               + 2 * kKeys * 4                 // pages of a unit's keys, 2 units
+                               + 256 + 2 * 128 * 4;            // barriers, TMEM base; exchange
   static constexpr int kUsed = kQ + kSlots * kSlot + kTail;
   static constexpr int kSmem = kUsed > 120 * 1024 ? kUsed : 120 * 1024;      // one CTA an SM: each takes all of TMEM
   static_assert(kSmem <= 232448);
@@ -85,19 +86,12 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-// 16 columns of this warp's lanes; the registers hold them after tmem_arrived on them.
-__device__ __forceinline__ void tmem_fetch(uint32_t taddr, uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
 }
 
 // Barrier among `n` threads that tells each whether all came with `v`.
@@ -114,13 +108,44 @@ __device__ __forceinline__ bool barrier_and(int id, int n, bool v) {
   return r != 0;
 }
 
+__device__ __forceinline__ bool barrier_or(int id, int n, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.u32 p, %3, 0;\n"
+      "barrier.cta.red.or.aligned.pred q, %1, %2, p;\n"
+      "selp.u32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)v) : "memory");
+  return r != 0;
+}
+
 // Byte offset of a 16-byte chunk of row `row`, 64 features a block of `rows` rows.
 __device__ __forceinline__ int tile_at(int rows, int row, int chunk) {
   return (chunk >> 3) * rows * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
 }
 
+__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
+}
+
+template <typename T> __device__ __forceinline__ T pack_nan() {
+  const uint32_t w = pack2of<T>(__int_as_float(0x7fffffff), 0.f);
+  return *reinterpret_cast<const T*>(&w);
+}
+
+// What the producers tell the others of a unit: {first key, flags, first token of the request, head}, {first row of the item, rows of
+// the request, position of its first token, units of the item behind this one}.
+constexpr int kBegins = 1, kEnds = 2, kTwo = 4, kWholeStart = 8;   // first unit of its item in this share; last one of the item; rows
+                                                                   // in both tiles; the item's first unit is in this share
+
 template <typename T, int STORE, int DIM>
-__global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
+__global__ void __launch_bounds__(kThreads, 1)
+attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p) {
   using L = Layout<STORE, DIM>;
   constexpr bool k8 = L::k8;
   using M = std::conditional_t<k8, __half, T>;                 // type of the products
@@ -131,44 +156,47 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
   uint8_t* ring = smem + L::kQ;
   uint8_t* tail = ring + kSlots * L::kSlot;
   uint32_t* there = reinterpret_cast<uint32_t*>(tail);                       // [4][4]
-  float* scales = reinterpret_cast<float*>(tail + 64);                       // [4][2][kKeys]: key scale, value scale
+  int4* units = reinterpret_cast<int4*>(tail + 64);                          // [4][2], see below
+  float* scales = reinterpret_cast<float*>(tail + 192);                       // [4][2][kKeys]: key scale, value scale
   float* row_scales = scales + 4 * 2 * kKeys;                                // [2][kRows]
-  uint32_t* places = reinterpret_cast<uint32_t*>(tail + 64 + (k8 ? 4 * 2 * kKeys * 4 + 2 * kRows * 4 : 0));  // [2][2][kKeys]: keys', values' rows in 16 bytes
-  uint64_t* bars = reinterpret_cast<uint64_t*>(places + 4 * kKeys);
+  int* pages = reinterpret_cast<int*>(tail + 192 + (k8 ? 4 * 2 * kKeys * 4 + 2 * kRows * 4 : 0));   // [2][kKeys]: of a unit's keys, -1: none
+  uint64_t* bars = reinterpret_cast<uint64_t*>(pages + 2 * kKeys);
+  float* exchange = reinterpret_cast<float*>(bars + 32);                     // [2][128]: between the two threads of a row
   uint64_t *full = bars, *empty = bars + 5, *q_full = bars + 10, *q_empty = bars + 11, *s_full = bars + 12, *p_ready = bars + 14,
-           *o_full = bars + 16, *drained = bars + 18;                        // 19 barriers
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
+           *o_full = bars + 16, *drained = bars + 18, *partly = bars + 19;   // 20 barriers
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 20);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, kProducers); mbar_init(empty + i, 1); }
+    for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, k8 ? kProducers : 1); mbar_init(empty + i, 1); }
     mbar_init(q_full, kProducers);
     mbar_init(q_empty, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(s_full + i, 1); mbar_init(p_ready + i, 4); mbar_init(o_full + i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(s_full + i, 1); mbar_init(p_ready + i, 8); mbar_init(o_full + i, 1); }
     mbar_init(drained, 1);
+    mbar_init(partly, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   wait_for_previous_kernel();
   Cursor<kRows, kKeys> at;
   long long first, per;
-  const int count = find_share<kRows, kKeys, kThreads>(p, at, first, per, reinterpret_cast<long long*>(places));
+  const int count = find_share<kRows, kKeys, kThreads>(p, at, first, per, reinterpret_cast<long long*>(pages));
   const int share = blockIdx.x;
   if (count <= 0) {
     if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
     launch_dependents_now();
     return;
   }
-  if (warp == 11) tmem_alloc(tmem_slot, 512);
+  if (warp == kSoftmaxWarps) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   constexpr uint32_t kO = 256;                                 // first column of O; tile x: S at 128 x, O at kO + 128 x
 
-  if (warp >= 8 && warp < 11) {
+  if (warp > kSoftmaxWarps) {
     // ---------------- producers ----------------
-    const int t = tid - 8 * 32, wp = warp - 8;
+    const int t = tid - (kSoftmaxWarps + 1) * 32, wp = warp - kSoftmaxWarps - 1;
     uint64_t* waiting[3] = {nullptr, nullptr, nullptr};        // barriers of copies that are under way, the oldest last
     auto close = [&](uint64_t* bar) {                          // the copies so far belong to `bar`
       copies_close();
@@ -197,8 +225,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
     bool ok = true, fresh = true;
     [[maybe_unused]] int items = 0;
     auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
-    int page[2] = {-1, -1};
-    auto look_up = [&] {                                       // pages of this thread's keys of the unit at `at`
+    int page[2] = {-1, -1};                                    // of keys t and, in the first warp, t + 96
+    bool whole_start = false;
+    auto look_up = [&] {                                       // of the unit at `at`
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int key = at.key + t + i * kProducers;
@@ -206,60 +235,147 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         page[i] = mine ? p.t.table[at.b * p.t.table_ld + (key >> p.c.page_shift)] : -1;
       }
     };
-    auto spot_of = [&](long long page_ld, int page, int row) {
-      return (uint32_t)((unsigned long long)(page * page_ld + (long long)row * DIM) / (16 / (L::kRow / DIM)));
-    };
-    look_up();
-    for (int u = 0; u < count; ++u) {
-      if (fresh) {                                             // `at` is at unit u here: its queries
-        ok = ok && acquire(q_empty, q_phase);
-        q_phase ^= 1u;
-        constexpr int kChunks = DIM / 8, kAtOnce = 32 / kChunks;
-        const int chunk = lane % kChunks;
+    auto queries = [&] {                                       // of the item at `at`
+      ok = ok && acquire(q_empty, q_phase);
+      q_phase ^= 1u;
+      constexpr int kChunks = DIM / 8, kAtOnce = 32 / kChunks;
+      const int chunk = lane % kChunks;
 #pragma unroll 4
-        for (int row0 = wp * kAtOnce; row0 < kRows; row0 += 3 * kAtOnce) {
-          const int row = row0 + lane / kChunks, r = at.tile * kRows + row;
-          const bool in = row < kRows, is = ok && in && r < at.r.rows;
-          const T* q = static_cast<const T*>(p.q) + (is ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM + chunk * 8 : 0);
-          uint8_t* to = smem + (row >> 7) * (128 * DIM * 2) + tile_at(128, row & 127, chunk);
-          if constexpr (!kConvert) {
-            if (in) copy16(smem_u32(to), q, is);
-          } else {
-            uint4 w = is ? *reinterpret_cast<const uint4*>(q) : make_uint4(0u, 0u, 0u, 0u);
-            float most = largest_of(w.x, largest_of(w.y, largest_of(w.z, largest_of(w.w, 0.f))));
+      for (int row0 = wp * kAtOnce; row0 < kRows; row0 += kCopyWarps * kAtOnce) {
+        const int row = row0 + lane / kChunks, r = at.tile * kRows + row;
+        const bool in = row < kRows, is = ok && in && r < at.r.rows;
+        const T* q = static_cast<const T*>(p.q) + (is ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM + chunk * 8 : 0);
+        uint8_t* to = smem + (row >> 7) * (128 * DIM * 2) + tile_at(128, row & 127, chunk);
+        if constexpr (!kConvert) {
+          if (in) copy16(smem_u32(to), q, is);
+        } else {
+          uint4 w = is ? *reinterpret_cast<const uint4*>(q) : make_uint4(0u, 0u, 0u, 0u);
+          float most = largest_of(w.x, largest_of(w.y, largest_of(w.z, largest_of(w.w, 0.f))));
 #pragma unroll
-            for (int o = kChunks / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-            const float f = power_for(most);
-            if (in) {
-              *reinterpret_cast<uint4*>(to) = make_uint4(to_half(w.x, f), to_half(w.y, f), to_half(w.z, f), to_half(w.w, f));
-              if (chunk == 0) row_scales[items * kRows + row] = inverse_power(f);
-            }
+          for (int o = kChunks / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+          const float f = power_for(most);
+          if (in) {
+            *reinterpret_cast<uint4*>(to) = make_uint4(to_half(w.x, f), to_half(w.y, f), to_half(w.z, f), to_half(w.w, f));
+            if (chunk == 0) row_scales[items * kRows + row] = inverse_power(f);
           }
         }
-        items ^= 1;
-        close(q_full);
       }
-      // places of the unit's keys: a thread has key t, the first warp the last 32 too; the pages of the next unit's keys are under
-      // way meanwhile
-      uint32_t* place = places + (u & 1) * 2 * kKeys;
+      items ^= 1;
+      close(q_full);
+    };
+    if constexpr (!k8) {
+      if (wp > 0) {                                            // these two only help with the queries
+        for (int u = 0; u < count && ok; ++u) {
+          if (fresh) {
+            queries();
+            flush();
+          }
+          fresh = at.unit + 1 == at.units;
+          if (u + 1 < count) at.next(p);
+        }
+      } else {
+        const int mask = (1 << p.c.page_shift) - 1, shift = min(p.c.page_shift, 7), rows = 1 << shift, boxes = kKeys >> shift;
+        const int box = lane & 15, part = lane >> 4;           // this lane's box of a unit, and which 64 features of it
+        int page = -1;
+        auto look_up_box = [&] {                               // page of the box in the unit at `at`
+          const int key = at.key + (box << shift);
+          page = box < boxes && key < at.k.hi && key + rows > at.k.lo ? p.t.table[at.b * p.t.table_ld + (key >> p.c.page_shift)] : -1;
+          if ((unsigned)page >= (unsigned)p.c.pages) page = -1;
+        };
+        bool whole_start = false;
+        uint32_t part_phase = 0;
+        look_up_box();
+        for (int u = 0; u < count && ok; ++u) {
+          const bool begins = fresh;
+          if (begins) {
+            queries();
+            flush();
+            whole_start = at.unit == 0;
+          }
+          const int row0 = at.tile * kRows, key0 = at.key, page_row = (at.h << p.c.page_shift) + ((key0 + (box << shift)) & mask);
+          fresh = at.unit + 1 == at.units;
+          const int4 item[2] = {make_int4(key0, (begins ? kBegins : 0) | (fresh ? kEnds : 0) | (at.r.rows - row0 > 128 ? kTwo : 0) | (whole_start ? kWholeStart : 0), at.r.q0, at.h),
+                                make_int4(row0, at.r.rows, at.r.length - at.r.n, at.units - 1 - at.unit)};
+          const bool mine = page >= 0 && part < DIM / 64;
+          const int box_page = page;
+          uint32_t word[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = 32 * i + lane;
+            const int has = __shfl_sync(0xffffffffu, page, j >> shift);
+            word[i] = __ballot_sync(0xffffffffu, has >= 0 && key0 + j >= at.k.lo && key0 + j < at.k.hi);
+          }
+          const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * rows * 128;
+          if (u + 1 < count) {
+            at.next(p);
+            look_up_box();
+          }
+          // the words of unit u - 4 have been read: its products are done (the slot that this unit's keys take says so)
+          if (!(ok = mbar_wait(empty + slot, phase, abort_flag))) break;
+          if (lane == 0) {
+            *reinterpret_cast<uint4*>(there + (u & 3) * 4) = make_uint4(word[0], word[1], word[2], word[3]);
+            units[(u & 3) * 2] = item[0];
+            units[(u & 3) * 2 + 1] = item[1];
+            mbar_expect_tx(full + slot, bytes);
+          }
+          __syncwarp();
+          if (mine) tma_load_3d(smem_u32(ring + slot * L::kSlot) + part * (kKeys * 128) + (box << shift) * 128, &map_k, part * 64, page_row, box_page, full + slot);
+          next_slot();
+          if (!(ok = mbar_wait(empty + slot, phase, abort_flag))) break;
+          const bool all = (word[0] & word[1] & word[2] & word[3]) == 0xffffffffu;
+          uint64_t* bar = all ? full + slot : partly;
+          if (lane == 0) mbar_expect_tx(bar, bytes);
+          __syncwarp();
+          if (mine) tma_load_3d(smem_u32(ring + slot * L::kSlot) + part * (kKeys * 128) + (box << shift) * 128, &map_v, part * 64, page_row, box_page, bar);
+          if (!all) {                                          // values of keys that are not there: zeros, whatever memory holds
+            ok = mbar_wait(partly, part_phase, abort_flag);
+            part_phase ^= 1u;
+            if (!ok) break;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!((word[i] >> lane) & 1u))
+                for (int c = 0; c < DIM / 8; ++c)
+                  *reinterpret_cast<uint4*>(ring + slot * L::kSlot + (c >> 3) * (kKeys * 128) + (32 * i + lane) * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            fence_async_proxy();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + slot);
+          }
+          next_slot();
+        }
+        // copies under way end before their memory goes: the slots' barriers say so, also after a wait that gave up
+        for (int i = 0; i < kSlots && !ok; ++i) {
+          volatile int gave_up = 0;
+          mbar_wait_limited(full + i, 0, &gave_up, 1u << 16);
+          mbar_wait_limited(full + i, 1, &gave_up, 1u << 16);
+        }
+      }
+    } else {
+    look_up();
+    for (int u = 0; u < count; ++u) {
+      if (fresh) queries();
+      // pages of the unit's keys; those of the next unit's are under way meanwhile
+      int* unit_pages = pages + (u & 1) * kKeys;
+      const int mask = (1 << p.c.page_shift) - 1, key0 = at.key, first_row = at.h << p.c.page_shift;
       {
-        uint2 spot[2];
-        bool is[2];
+        int has[2];
         [[maybe_unused]] float ks[2] = {0.f, 0.f}, vs[2] = {1.f, 1.f};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int row = (at.h << p.c.page_shift) + ((at.key + t + i * kProducers) & ((1 << p.c.page_shift) - 1));
-          is[i] = (unsigned)page[i] < (unsigned)p.c.pages;
-          spot[i] = is[i] ? make_uint2(spot_of(p.c.k_page, page[i], row), spot_of(p.c.v_page, page[i], row)) : make_uint2(kNowhere, kNowhere);
+          has[i] = (unsigned)page[i] < (unsigned)p.c.pages ? page[i] : -1;
           if constexpr (k8) {
-            const long long w = (((long long)page[i] * p.c.heads) << p.c.page_shift) + row;
-            if (is[i]) {
+            const long long w = (((long long)has[i] * p.c.heads) << p.c.page_shift) + first_row + ((key0 + t + i * kProducers) & mask);
+            if (has[i] >= 0) {
               ks[i] = p.c.k_scale[w];
               vs[i] = p.c.v_scale[w];
             }
           }
         }
+        const int row0 = at.tile * kRows;
+        const bool begins = fresh;
+        if (begins) whole_start = at.unit == 0;
         fresh = at.unit + 1 == at.units;
+        const int4 item[2] = {make_int4(at.key, (begins ? kBegins : 0) | (fresh ? kEnds : 0) | (at.r.rows - row0 > 128 ? kTwo : 0) | (whole_start ? kWholeStart : 0), at.r.q0, at.h),
+                              make_int4(row0, at.r.rows, at.r.length - at.r.n, at.units - 1 - at.unit)};
         if (u + 1 < count) {
           at.next(p);
           look_up();
@@ -270,15 +386,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
         for (int i = 0; i < 2; ++i) {
           const int key = t + i * kProducers;
           if (i == 1 && wp != 0) break;
-          place[key] = spot[i].x;
-          place[kKeys + key] = spot[i].y;
-          const uint32_t word = __ballot_sync(0xffffffffu, is[i]);
+          unit_pages[key] = has[i];
+          const uint32_t word = __ballot_sync(0xffffffffu, has[i] >= 0);
           if (lane == 0) there[(u & 3) * 4 + (key >> 5)] = word;
           if constexpr (k8) {
             float* sc = scales + (u & 3) * 2 * kKeys;
             sc[key] = ks[i];
             sc[kKeys + key] = vs[i] < cache::kLeastScale ? cache::kLeastScale : vs[i];
           }
+        }
+        if (t == 0) {
+          units[(u & 3) * 2] = item[0];
+          units[(u & 3) * 2 + 1] = item[1];
         }
       }
       // all of them go on or none: a thread that has left would be waited for at the next barrier
@@ -287,27 +406,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
       for (int kv = 0; kv < 2; ++kv) {
         if (kv && !(ok = acquire(empty + slot, phase))) break;
         uint8_t* dst = ring + slot * L::kSlot;
-        constexpr int kChunks = L::kRow / 16, kAtOnce = 32 / kChunks, kPer = (kKeys / kAtOnce + 2) / 3;
+        constexpr int kChunks = L::kRow / 16, kAtOnce = 32 / kChunks, kPer = (kKeys / kAtOnce + kCopyWarps - 1) / kCopyWarps;
         const int chunk = lane % kChunks;
         const char* base = static_cast<const char*>(kv ? p.c.v : p.c.k) + chunk * 16;
-        auto row_of = [&](int i) { return (wp + 3 * i) * kAtOnce + lane / kChunks; };
-        uint32_t spot[kPer];                                   // read ahead: no load passes a copy
+        auto row_of = [&](int i) { return (wp + kCopyWarps * i) * kAtOnce + lane / kChunks; };
+        int has[kPer];                                         // read ahead: no load passes a copy
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) spot[i] = row_of(i) < kKeys ? place[kv * kKeys + row_of(i)] : kNowhere;
-        if constexpr (!k8) {
-          const uint32_t to = smem_u32(dst);
-#pragma unroll
-          for (int i = 0; i < kPer; ++i) {
-            const bool is = spot[i] != kNowhere;
-            if (i < kPer - 1 || row_of(i) < kKeys)
-              copy16(to + tile_at(kKeys, row_of(i), chunk), base + (is ? (unsigned long long)spot[i] * 16 : 0ull), is);
-          }
-          close(full + slot);
-        } else {
+        for (int i = 0; i < kPer; ++i) has[i] = row_of(i) < kKeys ? unit_pages[row_of(i)] : -1;
+        const long long page_bytes = (kv ? p.c.v_page : p.c.k_page) * (L::kRow / DIM);
+        auto source = [&](int i) { return base + has[i] * page_bytes + (long long)(first_row + ((key0 + row_of(i)) & mask)) * L::kRow; };
+        {
           uint4 raw[kPer];
 #pragma unroll
           for (int i = 0; i < kPer; ++i)
-            raw[i] = spot[i] != kNowhere ? *reinterpret_cast<const uint4*>(base + (unsigned long long)spot[i] * 16) : make_uint4(0u, 0u, 0u, 0u);
+            raw[i] = has[i] >= 0 ? *reinterpret_cast<const uint4*>(source(i)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
           for (int i = 0; i < kPer; ++i) {
             const int row = row_of(i);
@@ -329,11 +441,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
       }
     }
     flush();
-  } else if (warp == 11) {
+    }
+  } else if (warp == kSoftmaxWarps) {
     // ---------------- products ----------------
     const uint32_t qk = idesc<M>(kKeys, false), pv = idesc<M>(DIM, true);
-    int k_slot = 0, slot = 0;                                  // slot of the keys in S, next slot of the ring
-    uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0};
+    int slot = 0;
+    uint32_t phase = 0, q_phase = 0, p_phase = 0;
     bool ok = true;
     auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
     auto scores = [&](int x, int s) {
@@ -344,7 +457,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) umma_bf16(tmem + x * 128, a + 2 * k, b + 2 * k, qk, (h | k) != 0);
       }
-      umma_commit(s_full + x);
     };
     auto rows = [&](int x, int s, bool accumulate) {
       const uint64_t b = desc_mn(smem_u32(ring + s * L::kSlot));
@@ -352,62 +464,55 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
       for (int k = 0; k < kKeys / 16; ++k)
         mma_ts(tmem + kO + x * 128, tmem + x * 128 + 8 * k, b + k * (16 * 128 / 16), pv, accumulate || k != 0);
     };
-    bool fresh = true, opened = false;                         // the next unit begins an item; its scores are issued
+    bool opened = false;                                       // the unit's scores are issued
     for (int u = 0; u < count && ok; ++u) {
-      const bool two = at.r.rows - at.tile * kRows > 128;
-      const bool begins = fresh;
-      if (!opened) {
-        if (fresh) {
-          ok = mbar_wait(q_full, q_phase, abort_flag);
-          q_phase ^= 1u;
-        }
+      if (!opened) {                                           // it begins an item here
+        ok = mbar_wait(q_full, q_phase, abort_flag);
+        q_phase ^= 1u;
         ok = ok && mbar_wait(full + slot, phase, abort_flag);
         if (!ok) break;
         tc_fence_after();
         if (lane == 0) {
           scores(0, slot);
-          if (two) scores(1, slot);
+          umma_commit(s_full);
+          if (units[(u & 3) * 2].y & kTwo) scores(1, slot);
+          umma_commit(s_full + 1);                             // also without rows: the warps of the tile go from unit to unit
           umma_commit(empty + slot);
         }
-        k_slot = slot;
         next_slot();
       }
-      (void)k_slot;
-      opened = false;
-      const bool ends = at.unit + 1 == at.units, more = u + 1 < count && !ends;
+      const int flags = units[(u & 3) * 2].y;
+      const bool two = flags & kTwo, more = u + 1 < count && !(flags & kEnds);
       if (!more && lane == 0) umma_commit(q_empty);
       const int v_slot = slot;
       ok = mbar_wait(full + v_slot, phase, abort_flag);
       if (!ok) break;
       next_slot();
-      for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
-        ok = mbar_wait(p_ready + x, p_phase[x], abort_flag);
-        p_phase[x] ^= 1u;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        ok = ok && mbar_wait(p_ready + x, p_phase, abort_flag);
+        if (x == 0 && more) ok = ok && mbar_wait(full + slot, phase, abort_flag);
         if (!ok) break;
         tc_fence_after();
         if (lane == 0) {
-          rows(x, v_slot, !begins);
-          if (!more) umma_commit(o_full + x);
-          if (x == (two ? 1 : 0)) umma_commit(empty + v_slot);
-        }
-        if (more) {
-          if (x == 0) {
-            ok = mbar_wait(full + slot, phase, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
+          if (x == 0 || two) {
+            rows(x, v_slot, !(flags & kBegins));
+            if (!more) umma_commit(o_full + x);
           }
-          if (lane == 0) scores(x, slot);
+          if (x == 1) umma_commit(empty + v_slot);
+          if (more) {
+            if (x == 0 || two) scores(x, slot);
+            umma_commit(s_full + x);
+          }
         }
         __syncwarp();
       }
+      p_phase ^= 1u;
       if (more && ok) {
         if (lane == 0) umma_commit(empty + slot);
-        k_slot = slot;
         next_slot();
-        opened = true;
       }
-      fresh = ends;
-      if (u + 1 < count) at.next(p);
+      opened = more;
       __syncwarp();
     }
     // TMEM and the ring are free when every product has ended, also after a wait that gave up
@@ -417,160 +522,185 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
     __syncwarp();
   } else {
     // ---------------- softmax ----------------
-    const int x = warp >> 2, row = tid & 127;
-    const uint32_t s_at = tmem + x * 128 + ((uint32_t)(warp & 3) << 21), o_at = s_at + kO;
+    // tile, which half of the keys (and of the features of O), row
+    const int x = warp >> 3, half = (warp >> 2) & 1, row = tid & 127, pair = 2 + x * 4 + (warp & 3);
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+    const uint32_t s_at = tmem + lanes + x * 128, o_at = tmem + lanes + kO + x * 128 + half * (DIM / 2);
+    float* shared = exchange + x * 128 + row;
     float ref = 0.f, sum = 0.f, row_scale = 0.f;
-    int items = 1;                                             // items so far, the parity
-    bool unread = true;
-    int pos = -1;
-    int began = 0;                                             // the item's first unit, counted from the share's
-    bool fresh = true, ok = true, active = false;
+    int pos = -1, items = 0;                                   // position of the row's token; items so far, the parity
+    bool ok = true, active = false;
     uint32_t s_phase = 0, o_phase = 0;
+    if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
     for (int u = 0; u < count; ++u) {
-      const int r = at.tile * kRows + x * 128 + row;
-      if (fresh) {
-        fresh = false;
-        began = u - at.unit;
-        active = at.r.rows - at.tile * kRows > x * 128;
-        const bool is = r < at.r.rows;
-        pos = is ? at.r.length - at.r.n + r / p.group : -1;
-        ref = is ? -INFINITY : 0.f;                            // rows past the end never ask for a reference
-        items ^= 1;
-        unread = true;
-        sum = 0.f;
+      // the two warps of a row go on or give up together: they meet at barriers further down
+      ok = barrier_and(pair, 64, mbar_wait(s_full + x, s_phase, abort_flag));
+      if (!ok) {                                               // it gave up: the item at hand becomes NaN
+        const int4 first_half = units[((u - 1) & 3) * 2], item = units[((u - 1) & 3) * 2 + 1];
+        const int r = item.x + x * 128 + row;
+        if (u > 0 && !(first_half.y & kEnds) && r < item.y)
+          for (int e = half * (DIM / 2); e < (half + 1) * (DIM / 2); ++e)
+            static_cast<T*>(p.out)[token_of(p, first_half.z, r) * p.out_ld + (long long)head_of(p, first_half.w, r) * DIM + e] = pack_nan<T>();
+        break;
       }
-      if (active) {
-        ok = ok && mbar_wait(s_full + x, s_phase, abort_flag);
-        s_phase ^= 1u;
-        tc_fence_after();
+      s_phase ^= 1u;
+      tc_fence_after();
+      const int key = units[(u & 3) * 2].x, flags = units[(u & 3) * 2].y;
+      if (flags & kBegins) {
+        const int4 item = units[(u & 3) * 2 + 1];
+        const int r = item.x + x * 128 + row;
+        active = x == 0 || (flags & kTwo);
+        const bool is = r < item.y;
+        pos = is ? item.z + r / p.group : 0x7fffffff;          // no row: nothing to mask, no reference to look for
+        ref = is ? -INFINITY : 0.f;
+        sum = 0.f;
+        row_scale = kConvert ? row_scales[items * kRows + x * 128 + row] * p.scale_log2 : p.scale_log2;
+        items ^= 1;
+      }
+      if (!active) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_ready + x);
+      } else {
         const uint4 bits = *reinterpret_cast<const uint4*>(there + (u & 3) * 4);
-        const float* sc = scales + (u & 3) * 2 * kKeys;
-        if (unread) {                                          // the item's first unit: its queries are there
-          row_scale = kConvert ? row_scales[items * kRows + x * 128 + row] * p.scale_log2 : p.scale_log2;
-          unread = false;
-        }
+        const float* sc = scales + (u & 3) * 2 * kKeys + half * 64;
         // every row of the warp sees all keys of the unit
         const bool clear = (bits.x & bits.y & bits.z & bits.w) == 0xffffffffu &&
-                           __all_sync(0xffffffffu, pos < 0 ? r >= at.r.rows : at.key + kKeys - 1 <= pos && (p.window == 0 || at.key > pos - p.window));
-        const int lowest = p.window ? max(pos - p.window + 1, 0) : 0;
-        // bits of 32 keys that the row sees
+                           __all_sync(0xffffffffu, key + kKeys - 1 <= pos && (p.window == 0 || pos == 0x7fffffff || key > pos - p.window));
+        const int lowest = p.window && pos != 0x7fffffff ? max(pos - p.window + 1, 0) : 0;
+        // bits of 32 keys of this half that the row sees
         auto seen = [&](int c) {
-          const int k0 = at.key + 32 * c;
-          uint32_t see = c == 0 ? bits.x : c == 1 ? bits.y : c == 2 ? bits.z : bits.w;
+          const int k0 = key + 64 * half + 32 * c;
+          uint32_t see = half == 0 ? (c == 0 ? bits.x : bits.y) : (c == 0 ? bits.z : bits.w);
           see &= pos < k0 ? 0u : pos - k0 >= 31 ? 0xffffffffu : (2u << (pos - k0)) - 1u;
           see &= lowest <= k0 ? 0xffffffffu : lowest - k0 > 31 ? 0u : ~((1u << (lowest - k0)) - 1u);
           return see;
         };
-        uint32_t packed[64];
-        float more = 0.f, most = 0.f;                          // sums of the probabilities, without and with the values' scales
-        auto make = [&](float safe, auto masked) {
+        uint32_t packed[32];
+        float more, most;                                      // sums of the probabilities, without and with the values' scales
+        bool renew = __any_sync(0xffffffffu, ref == -INFINITY);  // the same in both halves
+        for (;;) {
+          if (renew) {                                         // new references, from the scores themselves
+            float best = ref;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              float v[16];
+              tmem_ld16(s_at + 64 * half + 16 * c, v);
+              const uint32_t see = seen(c / 2) >> (16 * (c & 1));
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const int at = 16 * c + e;
+                const float t = k8 ? v[e] * (sc[at] * row_scale) + log2f(sc[kKeys + at]) : v[e] * row_scale;
+                best = (see >> e) & 1u ? fmaxf(best, t) : best;
+              }
+            }
+            if (half) *shared = best;
+            named_barrier(pair, 64);
+            if (!half) *shared = best = fmaxf(best, *shared);
+            named_barrier(pair, 64);
+            if (half) best = *shared;
+            const float shrink = ref == -INFINITY ? 0.f : ex2(ref - best);
+            ref = best;
+            sum *= shrink;
+            if (!(flags & kBegins)) {                          // O holds earlier units' rows
+#pragma unroll 1
+              for (int c = 0; c < DIM / 32; ++c) {
+                float v[16];
+                tmem_ld16(o_at + 16 * c, v);
+                uint32_t w[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(v[e] * shrink);
+                tmem_st16(o_at + 16 * c, w);
+              }
+              tmem_st_wait();
+            }
+          }
+          const float safe = ref == -INFINITY ? 0.f : ref;
           const f32x2 low = pack2(-safe, -safe), by = pack2(row_scale, row_scale);
-          f32x2 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)}, most2 = pack2(0.f, 0.f);
-          uint32_t v[2][16];
-          tmem_fetch(s_at, v[0]);
-          tmem_arrived(v[0]);
-          uint32_t see = 0;
+          f32x2 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+          [[maybe_unused]] f32x2 most2 = pack2(0.f, 0.f);
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            if (c < 7) tmem_fetch(s_at + 16 * (c + 1), v[(c + 1) & 1]);
-            const uint32_t (&w)[16] = v[c & 1];
-            if constexpr (decltype(masked)::value) see = c & 1 ? see >> 16 : seen(c / 2);
+          for (int c = 0; c < 2; ++c) {
+            float v[32];
+            tmem_ld32(s_at + 64 * half + 32 * c, v);
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
+            for (int e = 0; e < 32; e += 4) {
               f32x2 f[2] = {by, by};
-              [[maybe_unused]] f32x2 g[2] = {by, by};
               if constexpr (k8) {
-                const float4 a = *reinterpret_cast<const float4*>(sc + 16 * c + e), b = *reinterpret_cast<const float4*>(sc + kKeys + 16 * c + e);
+                const float4 a = *reinterpret_cast<const float4*>(sc + 32 * c + e);
                 f[0] = mul2(pack2(a.x, a.y), by); f[1] = mul2(pack2(a.z, a.w), by);
+              }
+#pragma unroll
+              for (int i = 0; i < 4; i += 2) {
+                const float2 t = unpack2(fma2(pack2(v[e + i], v[e + i + 1]), f[i / 2], low));
+                v[e + i] = t.x;
+                v[e + i + 1] = t.y;
+              }
+            }
+            if (!clear) {
+              const uint32_t see = seen(c);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              [[maybe_unused]] f32x2 g[2];
+              if constexpr (k8) {
+                const float4 b = *reinterpret_cast<const float4*>(sc + kKeys + 32 * c + e);
                 g[0] = pack2(b.x, b.y); g[1] = pack2(b.z, b.w);
               }
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                float2 t = unpack2(fma2(pack2(__uint_as_float(w[e + 2 * i]), __uint_as_float(w[e + 2 * i + 1])), f[i], low));
-                if constexpr (decltype(masked)::value) {
-                  t.x = (see >> (e + 2 * i)) & 1u ? t.x : -INFINITY;
-                  t.y = (see >> (e + 2 * i + 1)) & 1u ? t.y : -INFINITY;
-                }
-                t.x = ex2(t.x);
-                t.y = ex2(t.y);
-                f32x2 t2 = pack2(t.x, t.y);
+                f32x2 t2 = pack2(ex2(v[e + 2 * i]), ex2(v[e + 2 * i + 1]));
                 sum2[i] = add2(sum2[i], t2);
                 if constexpr (k8) {
                   t2 = mul2(t2, g[i]);
                   most2 = add2(most2, t2);
-                  t = unpack2(t2);
                 }
-                packed[8 * c + e / 2 + i] = pack2of<M>(t.x, t.y);
+                const float2 t = unpack2(t2);
+                packed[16 * c + e / 2 + i] = pack2of<M>(t.x, t.y);
               }
             }
-            if (c < 7) tmem_arrived(v[(c + 1) & 1]);
           }
           const float2 a = unpack2(add2(sum2[0], sum2[1])), b = unpack2(most2);
           more = a.x + a.y;
           most = k8 ? b.x + b.y : more;
-        };
-        bool again = __any_sync(0xffffffffu, ref == -INFINITY);
-        if (!again) {
-          if (clear) make(ref, std::false_type());
-          else make(ref, std::true_type());
-          again = __any_sync(0xffffffffu, most > kMost);
-        }
-        if (again) {                                           // new references, from the scores themselves
-          float best = ref;
-#pragma unroll 1
-          for (int c = 0; c < 8; ++c) {
-            float v[16];
-            tmem_ld16(s_at + 16 * c, v);
-            const uint32_t see = seen(c / 2) >> (16 * (c & 1));
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int key = 16 * c + e;
-              const float t = k8 ? v[e] * (sc[key] * row_scale) + log2f(sc[kKeys + key]) : v[e] * row_scale;
-              best = (see >> e) & 1u ? fmaxf(best, t) : best;
-            }
-          }
-          const float shrink = ref == -INFINITY ? 0.f : ex2(ref - best);
-          ref = best;
-          sum *= shrink;
-          if (u > max(began, 0)) {                             // O holds earlier units' rows
-#pragma unroll 1
-            for (int c = 0; c < DIM / 32; ++c) {
-              float v[32];
-              tmem_ld32(o_at + 32 * c, v);
-              uint32_t w[32];
-#pragma unroll
-              for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(v[e] * shrink);
-              tmem_st32(o_at + 32 * c, w);
-            }
-            tmem_st_wait();
-          }
-          make(ref == -INFINITY ? 0.f : ref, std::true_type());
+          // both halves of the rows alike; and both have read their scores, over which the probabilities are written
+          const bool over = barrier_or(pair, 64, most > kMost);
+          if (renew || !over) break;
+          renew = true;
         }
         sum += more;
-        tmem_st32(s_at, packed);
-        tmem_st32(s_at + 32, packed + 32);
+        tmem_st32(s_at + 32 * half, packed);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(p_ready + x);
       }
-      const bool last = at.unit + 1 == at.units;
-      if (last || u + 1 == count) {
-        const bool whole = last && began >= 0;
+      if ((flags & kEnds) || u + 1 == count) {
+        const int4 item = units[(u & 3) * 2 + 1];
+        const bool whole = (flags & kEnds) && (flags & kWholeStart);
+        const int q0 = units[(u & 3) * 2].z, h = units[(u & 3) * 2].w;
         if (active) {
-          ok = ok && mbar_wait(o_full + x, o_phase, abort_flag);
+          ok = mbar_wait(o_full + x, o_phase, abort_flag);
           o_phase ^= 1u;
           tc_fence_after();
-          const bool is = r < at.r.rows;
+          const int r = item.x + x * 128 + row;
+          const bool is = r < item.y;
+          float total = sum;
+          if (half) *shared = sum;
+          named_barrier(pair, 64);
+          if (!half) *shared = total = sum + *shared;
+          named_barrier(pair, 64);
+          if (half) total = *shared;
           // a wait that gave up leaves NaN
-          const float inv = !ok ? __int_as_float(0x7fffffff) : sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
-          const long long token = is ? token_of(p, at.r.q0, r) : 0;
-          const int qh = is ? head_of(p, at.h, r) : 0;
-          T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM;
-          float* slot = p.part + (2 * share + (began >= 0)) * (long long)(kRows * (DIM + 2));
+          const float inv = !ok ? __int_as_float(0x7fffffff) : total > 0.f ? 1.f / total : (total == total ? 0.f : total);
+          const long long token = is ? token_of(p, q0, r) : 0;
+          const int qh = is ? head_of(p, h, r) : 0;
+          T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM + half * (DIM / 2);
+          float* slot = p.part + (2 * share + ((flags & kWholeStart) != 0)) * (long long)(kRows * (DIM + 2));
           const int in = x * 128 + row;
 #pragma unroll 1
-          for (int c = 0; c < DIM / 32; ++c) {
+          for (int c = 0; c < DIM / 64; ++c) {
             float v[32];
             tmem_ld32(o_at + 32 * c, v);
             if (is && whole) {
@@ -580,35 +710,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_wide_kernel(Params p) {
                                                                          pack2of<T>(v[e + 4] * inv, v[e + 5] * inv), pack2of<T>(v[e + 6] * inv, v[e + 7] * inv));
             } else if (is) {
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(slot + in * DIM + 32 * c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+              for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(slot + in * DIM + half * (DIM / 2) + 32 * c + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
             }
             __syncwarp();
           }
-          if (is) {
+          if (is && half == 0) {
             if (!whole) {
               slot[kRows * DIM + in] = ref;
-              slot[kRows * (DIM + 1) + in] = ok ? sum : inv;
+              slot[kRows * (DIM + 1) + in] = ok ? total : inv;
             } else if (p.lse) {
-              p.lse[token * p.q_heads + qh] = ok ? 0.69314718055994531f * ((ref == -INFINITY ? 0.f : ref) + log2f(sum)) : inv;
+              p.lse[token * p.q_heads + qh] = ok ? 0.69314718055994531f * ((ref == -INFINITY ? 0.f : ref) + log2f(total)) : inv;
             }
           }
           tc_fence_before();
         }
         if (u + 1 == count && tid == 0) {
-          const bool open = !last && began >= 0;
-          const long long end = first + began + at.units - 1;
-          p.open[2 * share] = make_int4(at.r.q0, at.h, at.tile * kRows, min(kRows, at.r.rows - at.tile * kRows));
-          p.open[2 * share + 1] = make_int4(open ? (int)(end / per) : -1, 0, 0, 0);
+          const bool open = !(flags & kEnds) && (flags & kWholeStart);
+          p.open[2 * share] = make_int4(q0, h, item.x, min(kRows, item.y - item.x));
+          p.open[2 * share + 1] = make_int4(open ? (int)((first + u + item.w) / per) : -1, 0, 0, 0);
         }
-        fresh = true;
       }
-      if (u + 1 < count) at.next(p);
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 11) tmem_dealloc(tmem, 512);
+  if (warp == kSoftmaxWarps) tmem_dealloc(tmem, 512);
   launch_dependents_now();
 }
 

@@ -35,14 +35,24 @@ struct Tokens {
 constexpr int kThreads = 256;
 constexpr float kLeastScale = 7.888609052210118e-31f;   // 2^-100
 
+// Last of the `batch` segments that begins at or before i, by ascending first elements: seven of them looked at together, so that a
+// few hundred segments take three dependent loads.
+__device__ __forceinline__ int segment_of(const int* offsets, int batch, int i) {
+  int lo = 0, n = batch;                 // it is among lo .. lo + n - 1
+  while (n > 1) {
+    const int step = (n + 7) / 8;
+    int before = 0;
+#pragma unroll
+    for (int j = 1; j < 8; ++j) before += j * step < n && offsets[lo + j * step] <= i;
+    lo += before * step;
+    n = min(step, n - before * step);
+  }
+  return lo;
+}
 // Request of token i, or -1 where it belongs to none.
 __device__ __forceinline__ int request_of(const Tokens& t, int i) {
-  int lo = 0, hi = t.batch - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.offsets[mid] <= i) lo = mid; else hi = mid - 1;
-  }
-  return t.offsets[lo] <= i && i < t.offsets[lo + 1] ? lo : -1;
+  const int b = segment_of(t.offsets, t.batch, i);
+  return t.offsets[b] <= i && i < t.offsets[b + 1] ? b : -1;
 }
 // Row (page * heads + head) * page_size + place of token i of request b; page -1 where it has no place in the cache.
 __device__ __forceinline__ int page_of(const Tokens& t, const Pages& c, int b, int i, int& place) {
@@ -98,55 +108,73 @@ __device__ __forceinline__ float quotient_sticky(float x, float s) {
 // value 27.8 k tokens x 8 heads x 128 features took 132 us, and with one where it is close 178.
 //  int8: the rest of the nearest step k, a multiple of half a unit in the last place of s below s, is exact in float32.
 //  e4m3: 20 of the 23 bits go, a border is a half of the last that stays; below the normal numbers the quotient itself is taken.
+// Either is looked for in all eight values at once and mended in a branch that few warps take.
 template <int STORE>
 __device__ __forceinline__ uint2 held8(const float (&x)[8], float s) {
-  const float inv = __frcp_rn(s), half = 0.5f * s;
+  const float inv = __frcp_rn(s);
   uint2 r = make_uint2(0u, 0u);
   if constexpr (STORE == kInt8) {
+    constexpr float kMagic = 12582912.f;             // 1.5 * 2^23: the sum's last bits are the rounded number
+    const float half = 0.5f * s;
+    float m[8], most = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      constexpr float kMagic = 12582912.f;           // 1.5 * 2^23: the sum's last bits are the rounded number
-      const float m = x[i] * inv + kMagic, k = m - kMagic, rest = fmaf(-k, s, x[i]);
-      int held = (int)__float_as_uint(m);
-      if (fabsf(rest) >= half && (fabsf(rest) > half || (held & 1))) held += rest > 0.f ? 1 : -1;
-      (i < 4 ? r.x : r.y) |= ((unsigned)held & 0xffu) << (8 * (i & 3));
+      m[i] = fmaf(x[i], inv, kMagic);
+      most = fmaxf(most, fabsf(fmaf(kMagic - m[i], s, x[i])));
+    }
+    if (most >= half) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float rest = fmaf(kMagic - m[i], s, x[i]);
+        if (fabsf(rest) > half || (fabsf(rest) == half && (__float_as_uint(m[i]) & 1u))) m[i] += rest > 0.f ? 1.f : -1.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t a = __byte_perm(__float_as_uint(m[4 * i]), __float_as_uint(m[4 * i + 1]), 0x0040);
+      const uint32_t b = __byte_perm(__float_as_uint(m[4 * i + 2]), __float_as_uint(m[4 * i + 3]), 0x0040);
+      (i ? r.y : r.x) = __byte_perm(a, b, 0x5410);
     }
   } else {
+    float t[8], least = 1.f;
+    uint32_t near = 0xffffffffu;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      float t[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float v = x[i + j];
-        t[j] = v * inv;
-        const uint32_t bits = __float_as_uint(t[j]);
-        if (((bits + 8u) & 0xfffffu) - 0x80000u <= 16u) {
-          const uint32_t border = (bits + 8u) & 0xfff00000u | 0x80000u;
-          const float rest = fmaf(-__uint_as_float(border), s, v);
-          t[j] = __uint_as_float(rest == 0.f ? border : (rest > 0.f) == (v > 0.f) ? border + 1u : border - 1u);
-        }
-        if (fabsf(t[j]) < 0.015625f && v != 0.f) t[j] = quotient_sticky(v, s);
-      }
-      const unsigned two = __nv_cvt_float2_to_fp8x2(make_float2(t[0], t[1]), __NV_SATFINITE, __NV_E4M3);
-      (i < 4 ? r.x : r.y) |= two << (8 * (i & 3));
+    for (int i = 0; i < 8; ++i) {
+      t[i] = x[i] * inv;
+      least = fminf(least, fabsf(t[i]));
+      near = min(near, (__float_as_uint(t[i]) + 0x80008u) & 0xfffffu);
     }
+    if (near <= 16u || least < 0.015625f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = __float_as_uint(t[i]);
+        if (((bits + 0x80008u) & 0xfffffu) <= 16u) {
+          const uint32_t border = (bits + 8u) & 0xfff00000u | 0x80000u;
+          const float rest = fmaf(-__uint_as_float(border), s, x[i]);
+          t[i] = __uint_as_float(rest == 0.f ? border : (rest > 0.f) == (x[i] > 0.f) ? border + 1u : border - 1u);
+        }
+        if (fabsf(t[i]) < 0.015625f && x[i] != 0.f) t[i] = quotient_sticky(x[i], s);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i += 2)
+      (i < 4 ? r.x : r.y) |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(t[i], t[i + 1]), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
   }
   return r;
 }
 
-// A warp takes kPasses times as many neighbouring (token, head) rows as its lanes cover with 16 bytes each.  Every lane finds the
-// place of one row, so the chain of look-ups (request, length, page) is gone through once per warp, then all rows' loads are in
-// flight together.
+// A warp takes several times as many neighbouring (token, head) rows as its lanes cover with 16 bytes each.  Every lane finds the
+// place of one row, so the chain of look-ups (request, length, page) is gone through once per warp.
 constexpr int kPasses = 4;
 struct Spot {
   int page, row, source;       // page -1: none; row (head * page_size + place) in it; row of the dense side
 };
-__device__ __forceinline__ Spot spot_of(const Tokens& t, const Pages& c, long long unit, int n, const int* rows, const int* row_offsets,
+__device__ __forceinline__ Spot spot_of(const Tokens& t, const Pages& c, int unit, int n, const int* rows, const int* row_offsets,
                                         int source_rows) {
   Spot s{-1, 0, -1};
-  const long long i64 = unit / c.heads;
-  if (i64 >= n) return s;
-  const int i = (int)i64, head = (int)(unit % c.heads), b = request_of(t, i);
+  const int i = unit / c.heads, head = unit % c.heads;
+  if (i >= n) return s;
+  const int b = request_of(t, i);
   if (b < 0) return s;
   int place;
   s.page = page_of(t, c, b, i, place);
@@ -172,62 +200,62 @@ struct WriteParams {
   const int* rows;               // [n] source row of each token inside its request, or null: row i is token i
   const int* row_offsets;        // [batch + 1] first source row of each request
   int source_rows;
+  int passes;                    // 1 or kPasses
 };
 
 // Eight features a lane: one 16-byte load (two for float32).
 template <typename T, int STORE, int DIM>
 __global__ void __launch_bounds__(kThreads) write_kernel(WriteParams p) {
-  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes, kAtOnce = 2;
-  const int lane = threadIdx.x & 31, sub = lane / kLanes, feature = lane % kLanes * 8;
-  const long long unit0 = ((long long)blockIdx.x * (kThreads / 32) + warp_index()) * (kRows * kPasses);
-  Spot mine = lane < kRows * kPasses ? spot_of(p.t, p.c, unit0 + lane, p.n, p.rows, p.row_offsets, p.source_rows) : Spot{-1, 0, -1};
+  constexpr int kLanes = DIM / 8, kRows = 32 / kLanes;
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, feature = lane % kLanes * 8, mine = kRows * p.passes;
+  const int unit0 = (blockIdx.x * (kThreads / 32) + warp_index()) * mine;
+  wait_for_previous_kernel();
+  const Spot spot = lane < mine ? spot_of(p.t, p.c, unit0 + lane, p.n, p.rows, p.row_offsets, p.source_rows) : Spot{-1, 0, -1};
+  struct Raw { uint4 w[2][sizeof(T) / 2]; } raw{};             // a key's and a value's eight features
+  auto fetch = [&](const Spot& s) {
+    if (s.page < 0) return;
+    const int head = s.row >> p.c.page_shift;
+    const uint4* k = reinterpret_cast<const uint4*>(static_cast<const T*>(p.k) + s.source * p.k_ld + head * DIM + feature);
+    const uint4* v = reinterpret_cast<const uint4*>(static_cast<const T*>(p.v) + s.source * p.v_ld + head * DIM + feature);
 #pragma unroll
-  for (int first = 0; first < kPasses; first += kAtOnce) {
-    float x[kAtOnce][2][8];
-    Spot s[kAtOnce];
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) { raw.w[0][i] = k[i]; raw.w[1][i] = v[i]; }
+  };
+  Spot s = handed(spot, sub);
+  fetch(s);
+  for (int first = 0; first < mine; first += kRows) {
+    float x[2][8];
 #pragma unroll
-    for (int a = 0; a < kAtOnce; ++a) {
-      const int r = (first + a) * kRows + sub;
-      s[a] = handed(mine, r);
-      const int head = (int)((unit0 + r) % p.c.heads);
-      if (s[a].page >= 0) {
-        load8f(static_cast<const T*>(p.k) + s[a].source * p.k_ld + head * DIM + feature, x[a][0]);
-        load8f(static_cast<const T*>(p.v) + s[a].source * p.v_ld + head * DIM + feature, x[a][1]);
-      } else {
+    for (int kv = 0; kv < 2; ++kv) load8f(reinterpret_cast<const T*>(raw.w[kv]), x[kv]);
+    const Spot next = first + kRows < mine ? handed(spot, first + kRows + sub) : Spot{-1, 0, -1};
+    fetch(next);                 // under way while this row is worked on
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[a][0][e] = x[a][1][e] = 0.f;
+    for (int kv = 0; kv < 2; ++kv) {
+      void* base = kv ? p.c.v : p.c.k;
+      const long long at = s.page * (kv ? p.c.v_page : p.c.k_page) + (long long)s.row * DIM + feature;
+      if constexpr (STORE >= kE4M3) {
+        float top = 0.f;
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          top = fmaxf(top, fabsf(x[kv][e]));
+          bad |= x[kv][e] != x[kv][e];
+        }
+        if (bad) top = INFINITY;
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const bool finite = top <= 3.402823466e38f;
+        const float scale = finite ? fmaxf(__fdiv_rn(top, STORE == kE4M3 ? 448.f : 127.f), kLeastScale) : __int_as_float(0x7fffffff);
+        if (s.page >= 0) {
+          *reinterpret_cast<uint2*>(static_cast<unsigned char*>(base) + at) = finite ? held8<STORE>(x[kv], scale) : make_uint2(0u, 0u);
+          if (feature == 0) (kv ? p.c.v_scale : p.c.k_scale)[(((long long)s.page * p.c.heads) << p.c.page_shift) + s.row] = scale;
+        }
+      } else if (s.page >= 0) {
+        if constexpr (STORE == kF32) store8f(static_cast<float*>(base) + at, x[kv]);
+        else if constexpr (STORE == kBF16) store8f(static_cast<__nv_bfloat16*>(base) + at, x[kv]);
+        else store8f(static_cast<__half*>(base) + at, x[kv]);
       }
     }
-#pragma unroll
-    for (int a = 0; a < kAtOnce; ++a)
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        const int page = s[a].page;
-        void* base = kv ? p.c.v : p.c.k;
-        const long long at = page * (kv ? p.c.v_page : p.c.k_page) + (long long)s[a].row * DIM + feature;
-        if constexpr (STORE >= kE4M3) {
-          float top = 0.f;
-          bool bad = false;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            top = fmaxf(top, fabsf(x[a][kv][e]));
-            bad |= x[a][kv][e] != x[a][kv][e];
-          }
-          if (bad) top = INFINITY;
-#pragma unroll
-          for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const bool finite = top <= 3.402823466e38f;
-          const float scale = finite ? fmaxf(__fdiv_rn(top, STORE == kE4M3 ? 448.f : 127.f), kLeastScale) : __int_as_float(0x7fffffff);
-          if (page >= 0) {
-            *reinterpret_cast<uint2*>(static_cast<unsigned char*>(base) + at) = finite ? held8<STORE>(x[a][kv], scale) : make_uint2(0u, 0u);
-            if (feature == 0) (kv ? p.c.v_scale : p.c.k_scale)[(((long long)page * p.c.heads) << p.c.page_shift) + s[a].row] = scale;
-          }
-        } else if (page >= 0) {
-          if constexpr (STORE == kF32) store8f(static_cast<float*>(base) + at, x[a][kv]);
-          else if constexpr (STORE == kBF16) store8f(static_cast<__nv_bfloat16*>(base) + at, x[a][kv]);
-          else store8f(static_cast<__half*>(base) + at, x[a][kv]);
-        }
-      }
+    s = next;
   }
 }
 
@@ -283,7 +311,8 @@ __global__ void __launch_bounds__(kThreads) read_kernel(ReadParams p) {
   constexpr int E = STORE >= kE4M3 ? 16 : STORE == kF32 ? 4 : 8, kBytes = 16 / E;
   constexpr int kLanes = DIM / E, kRows = 32 / kLanes;
   const int lane = threadIdx.x & 31, sub = lane / kLanes, feature = lane % kLanes * E;
-  const long long unit0 = ((long long)blockIdx.x * (kThreads / 32) + warp_index()) * (kRows * kPasses);
+  const int unit0 = (blockIdx.x * (kThreads / 32) + warp_index()) * (kRows * kPasses);
+  wait_for_previous_kernel();
   Spot mine = lane < kRows * kPasses ? spot_of(p.t, p.c, unit0 + lane, p.n, nullptr, nullptr, 0) : Spot{-1, 0, -1};
   uint4 h[kPasses][2];
   [[maybe_unused]] float scale[kPasses][2];
@@ -308,7 +337,7 @@ __global__ void __launch_bounds__(kThreads) read_kernel(ReadParams p) {
     for (int kv = 0; kv < 2; ++kv) {
       float x[E];
       widen_held<STORE, E>(h[a][kv], scale[a][kv], x);
-      store_row<T, E>(static_cast<T*>(kv ? p.v : p.k) + (unit0 + a * kRows + sub) * DIM + feature, x);
+      store_row<T, E>(static_cast<T*>(kv ? p.v : p.k) + (long long)(unit0 + a * kRows + sub) * DIM + feature, x);
     }
   }
 }

@@ -481,23 +481,6 @@ int launch_single_nt(covspec_ctx* ctx, const T* A, const T* B, float* C, int m, 
 }
 
 // ---- tensor-core relevance path ----------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_tiled_fn() {
-  static EncodeTiledFn fn = [] {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      ptr = nullptr;
-    return reinterpret_cast<EncodeTiledFn>(ptr);
-  }();
-  return fn;
-}
-
 // Tensor map of a row-major bf16 matrix [rows, cols] with boxes of 64 columns (one 128-byte
 // swizzle row) by box_rows rows; out-of-range elements read as zero.
 int make_map_bf16(CUtensorMap* map, const void* base, long long rows, long long cols, int box_rows) {

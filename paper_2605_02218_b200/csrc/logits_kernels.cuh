@@ -7,9 +7,7 @@
 //   if w is not allowed: x = -inf
 // in float32, rounded once to the type of z.  Entries that none of it concerns are copied bit by bit.
 #pragma once
-#include <cuda_fp16.h>
-
-#include "common.cuh"
+#include "cache_kernels.cuh"
 
 namespace covspec {
 namespace edit {
@@ -76,18 +74,14 @@ __global__ void __launch_bounds__(kThreads) edit_kernel(Params p) {
   const int tid = threadIdx.x;
   int b = -1, b_end = 0, b_begin = 0;
   float r = 1.f, a = 0.f, f = 0.f;
+  wait_for_previous_kernel();
   auto mask_at = [&](const unsigned char* m, int i) { return !m ? 0xffu : i < len ? (unsigned)m[i / 8] >> (i % 8) : 0u; };
   unsigned ahead[kFlight];                 // the mask of this thread's first vectors of the row to come
 #pragma unroll
   for (int j = 0; j < kFlight; ++j) ahead[j] = mask_at(p.mask ? p.mask + row0 * p.mask_ld + seg0 / 8 : nullptr, (tid + j * kThreads) * kVec);
   for (int row = row0; row < row1; ++row) {
     if (b < 0 || row >= b_end) {          // the next request's tables
-      int lo = 0, hi = p.batch - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.row_offsets[mid] <= row) lo = mid; else hi = mid - 1;
-      }
-      b = lo;
+      b = cache::segment_of(p.row_offsets, p.batch, row);
       b_begin = max(p.row_offsets[b], 0);
       b_end = p.row_offsets[b + 1];
       if (row < b_begin || row >= b_end) {       // a row of no request stays as it was

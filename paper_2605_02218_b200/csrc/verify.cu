@@ -40,7 +40,7 @@ int check_cache(const covspec_cache* c) {
   if (c->store < COVSPEC_F32 || c->store > COVSPEC_INT8) return COVSPEC_ERR_ARG;
   if (c->store >= COVSPEC_E4M3 && (!c->k_scale || !c->v_scale)) return COVSPEC_ERR_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return COVSPEC_ERR_UNSUPPORTED;
-  if (c->page_size < 1 || c->page_size > 4096 || (c->page_size & (c->page_size - 1))) return COVSPEC_ERR_UNSUPPORTED;
+  if (c->page_size < 8 || c->page_size > 4096 || (c->page_size & (c->page_size - 1))) return COVSPEC_ERR_UNSUPPORTED;
   if (c->pages < 1 || c->heads < 1 || (long long)c->heads * c->page_size * c->head_dim > INT_MAX) return COVSPEC_ERR_SHAPE;
   const long long least = (long long)c->heads * c->page_size * c->head_dim;
   if (c->k_page_stride < least || c->v_page_stride < least) return COVSPEC_ERR_SHAPE;
@@ -93,10 +93,10 @@ int sm_count(int* sms) {
   return COVSPEC_OK;
 }
 
-// CTAs of the cache kernels for `rows` (token, head) rows of `lanes` lanes each.
-long long cache_grid(long long rows, int lanes) {
-  const long long per = (long long)(32 / lanes) * cache::kPasses * (cache::kThreads / 32);
-  return (rows + per - 1) / per;
+// CTAs of the cache kernels for `rows` (token, head) rows of `lanes` lanes each, `passes` times a warp's.
+int cache_grid(int rows, int lanes, int passes) {
+  const int per = (32 / lanes) * passes * (cache::kThreads / 32);
+  return (int)(((long long)rows + per - 1) / per);
 }
 
 // Largest request, as rows of a key head, that the attention kernel for few rows takes when both run; its CTAs at most per SM.
@@ -114,13 +114,34 @@ cudaError_t launch_rows(const attend::Params& prm, int ctas, cudaStream_t s) {
   return launch_dependent(attend::attend_join_kernel<T, ROWS, DIM>, dim3((unsigned)ctas, ROWS / 4), 128, 0, s, prm);
 }
 
+// The keys or the values of a 16-bit cache as [pages, heads * page_size, dim]: boxes of 64 features of a page's rows of one head, in
+// tiles of 128-byte rows with the 128-byte swizzle.
+bool make_page_map(CUtensorMap* map, const covspec_cache* c, const void* base, long long page_stride) {
+  EncodeTiledFn encode = encode_tiled_fn();
+  if (!encode) {
+    g_cuda_error = "cuTensorMapEncodeTiled is not available";
+    return false;
+  }
+  const cuuint64_t dims[3] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->heads * c->page_size, (cuuint64_t)c->pages};
+  const cuuint64_t strides[2] = {(cuuint64_t)c->head_dim * 2, (cuuint64_t)page_stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)std::min(c->page_size, 128), 1}, step[3] = {1, 1, 1};
+  const CUresult r = encode(map, c->store == COVSPEC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                            const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) g_cuda_error = "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r);
+  return r == CUDA_SUCCESS;
+}
+
 template <typename T, int STORE, int DIM>
-cudaError_t launch_wide(const attend::Params& prm, int ctas, cudaStream_t s) {
+cudaError_t launch_wide(const attend::Params& prm, const covspec_cache* cache, int ctas, cudaStream_t s) {
   constexpr auto kernel = attend::wide::attend_wide_kernel<T, STORE, DIM>;
   constexpr int smem = attend::wide::Layout<STORE, DIM>::kSmem, rows = attend::wide::kRows;
   cudaError_t e = allow_shared<kernel>(smem);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(kernel, dim3((unsigned)ctas), attend::wide::kThreads, smem, s, prm);
+  CUtensorMap map_k{}, map_v{};
+  if (STORE < cache::kE4M3 && (!make_page_map(&map_k, cache, cache->k, cache->k_page_stride) || !make_page_map(&map_v, cache, cache->v, cache->v_page_stride)))
+    return cudaErrorInvalidValue;
+  e = launch_dependent(kernel, dim3((unsigned)ctas), attend::wide::kThreads, smem, s, map_k, map_v, prm);
   if (e != cudaSuccess) return e;
   return launch_dependent(attend::attend_join_kernel<T, rows, DIM>, dim3((unsigned)ctas, rows / 4), 128, 0, s, prm);
 }
@@ -142,16 +163,20 @@ int covspec_cache_write(const covspec_cache* cache, const covspec_tokens* tokens
   if (!k || !v || !aligned16(k) || !aligned16(v)) return COVSPEC_ERR_ARG;
   if (k_stride < width || v_stride < width) return COVSPEC_ERR_SHAPE;
   if (k_stride * bytes_of(dtype) % 16 || v_stride * bytes_of(dtype) % 16) return COVSPEC_ERR_ARG;
-  const long long grid = cache_grid((long long)n * cache->heads, cache->head_dim / 8);
-  if (grid > INT_MAX) return COVSPEC_ERR_SHAPE;
-  cache::WriteParams prm{pages_of(cache), tokens_of(tokens), k, v, k_stride, v_stride, n, rows, row_offsets, source_rows};
+  if ((long long)n * cache->heads > INT_MAX / 2) return COVSPEC_ERR_SHAPE;
+  // few rows: one look-up and one row a lane group, for the latency (256 tokens x 8 heads 9.8 -> 4.6 us); many: the look-ups
+  // of four at a time (27.8 k tokens x 8 heads 84 -> 63 us)
+  int sms = 0;
+  if (const int e = sm_count(&sms)) return e;
+  const int one = cache_grid(n * cache->heads, cache->head_dim / 8, 1), passes = one <= 8 * sms ? 1 : cache::kPasses;
+  const int grid = passes == 1 ? one : cache_grid(n * cache->heads, cache->head_dim / 8, passes);
+  cache::WriteParams prm{pages_of(cache), tokens_of(tokens), k, v, k_stride, v_stride, n, rows, row_offsets, source_rows, passes};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   CUDA_TRY(with_type(dtype, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     return with_store(cache->store, [&](auto store) {
       return with_dim(cache->head_dim, [&](auto dim) {
-        cache::write_kernel<T, decltype(store)::value, decltype(dim)::value><<<(unsigned)grid, cache::kThreads, 0, s>>>(prm);
-        return cudaGetLastError();
+        return launch_dependent(cache::write_kernel<T, decltype(store)::value, decltype(dim)::value>, dim3((unsigned)grid), cache::kThreads, 0, s, prm);
       });
     });
   }));
@@ -166,16 +191,15 @@ int covspec_cache_read(const covspec_cache* cache, const covspec_tokens* tokens,
   if (n < 0) return COVSPEC_ERR_SHAPE;
   if (n == 0) return COVSPEC_OK;
   if (!k || !v || !aligned16(k) || !aligned16(v)) return COVSPEC_ERR_ARG;
-  const long long grid = cache_grid((long long)n * cache->heads, cache->head_dim * bytes_of(cache->store) / 16);
-  if (grid > INT_MAX) return COVSPEC_ERR_SHAPE;
+  if ((long long)n * cache->heads > INT_MAX / 2) return COVSPEC_ERR_SHAPE;
+  const int grid = cache_grid(n * cache->heads, cache->head_dim * bytes_of(cache->store) / 16, cache::kPasses);
   cache::ReadParams prm{pages_of(cache), tokens_of(tokens), k, v, n};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   CUDA_TRY(with_type(dtype, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     return with_store(cache->store, [&](auto store) {
       return with_dim(cache->head_dim, [&](auto dim) {
-        cache::read_kernel<T, decltype(store)::value, decltype(dim)::value><<<(unsigned)grid, cache::kThreads, 0, s>>>(prm);
-        return cudaGetLastError();
+        return launch_dependent(cache::read_kernel<T, decltype(store)::value, decltype(dim)::value>, dim3((unsigned)grid), cache::kThreads, 0, s, prm);
       });
     });
   }));
@@ -250,7 +274,7 @@ int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* token
       auto of_store = [&](auto store) {
         constexpr int kStore = decltype(store)::value;
         if (both)
-          if (const cudaError_t e = launch_wide<T, kStore, kDim>(wide, wide_ctas, s); e != cudaSuccess) return e;
+          if (const cudaError_t e = launch_wide<T, kStore, kDim>(wide, cache, wide_ctas, s); e != cudaSuccess) return e;
         return rows == 16 ? launch_rows<T, kStore, kDim, 16>(prm, ctas, s)
                : rows == 32 ? launch_rows<T, kStore, kDim, 32>(prm, ctas, s) : launch_rows<T, kStore, kDim, 64>(prm, ctas, s);
       };
@@ -287,7 +311,7 @@ int covspec_edit_logits(int logit_dtype, int rows, int vocab, long long ld, cons
   prm.segment = 4096;
   prm.group = 1;
   auto segments_of = [&] { return (unsigned)((vocab + prm.segment - 1) / prm.segment); };
-  while (prm.group < 16 && prm.group < rows && (long long)segments_of() * ((rows + 2 * prm.group - 1) / (2 * prm.group)) >= 4ll * sms) prm.group *= 2;
+  while (prm.group < 8 && prm.group < rows && (long long)segments_of() * ((rows + 2 * prm.group - 1) / (2 * prm.group)) >= 4ll * sms) prm.group *= 2;
   while (prm.segment > 2048 && (long long)segments_of() * rows < 2ll * sms) prm.segment /= 2;
   while ((rows + prm.group - 1) / prm.group > 65535) prm.group *= 2;
   const unsigned segments = segments_of();
@@ -298,8 +322,7 @@ int covspec_edit_logits(int logit_dtype, int rows, int vocab, long long ld, cons
     using T = std::remove_pointer_t<decltype(tag)>;
     const cudaError_t err = allow_shared<edit::edit_kernel<T>>(4096 / 8 + 4096 * 8);
     if (err != cudaSuccess) return err;
-    edit::edit_kernel<T><<<dim3(segments, (unsigned)groups), edit::kThreads, (size_t)smem, s>>>(prm);
-    return cudaGetLastError();
+    return launch_dependent(edit::edit_kernel<T>, dim3(segments, (unsigned)groups), edit::kThreads, (size_t)smem, s, prm);
   }));
   return COVSPEC_OK;
 }

@@ -205,7 +205,7 @@ class Paged:
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("store", ["f32", "bf16", "f16", "e4m3", "int8"])
-@pytest.mark.parametrize("heads,dim,page", [(1, 64, 1), (3, 128, 16), (8, 64, 64)])
+@pytest.mark.parametrize("heads,dim,page", [(1, 64, 8), (3, 128, 16), (8, 64, 64)])
 def test_written_rows_are_held_as_defined(dtype, store, heads, dim, page):
     new, length = [3, 0, 1, 40, 2], [3, 0, 17, 45, 1]             # the last one has a token without a position
     p = Paged(1, store, heads, dim, page, new, length, fill=False, apart=True)
@@ -292,7 +292,7 @@ def test_rows_at_the_ends_of_the_range(store):
 
 @pytest.mark.parametrize("store", ["f32", "bf16", "f16", "e4m3", "int8"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("heads,dim,page", [(2, 128, 16), (5, 64, 2)])
+@pytest.mark.parametrize("heads,dim,page", [(2, 128, 16), (5, 64, 8)])
 def test_read_gives_what_is_held(store, dtype, heads, dim, page):
     p = Paged(4, store, heads, dim, page, [5, 0, 30, 1], [9, 3, 30, 80], holes=[(2, 1, -1), (2, 0, 10 ** 6)])
     n = sum(p.new)
@@ -390,7 +390,7 @@ def test_single_tokens(dtype, store, dim, group):
 
 @pytest.mark.parametrize("dtype,store", KINDS)
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("heads,group,page", [(1, 8, 1), (3, 2, 32), (2, 1, 128)])
+@pytest.mark.parametrize("heads,group,page", [(1, 8, 8), (3, 2, 32), (2, 1, 128)])
 def test_blocks_of_every_size(dtype, store, dim, heads, group, page):
     new, length = [3, 1, 0, 8, 17, 5], [3, 130, 9, 100, 17, 64]
     p = Paged(21, store, heads, dim, page, new, length)
@@ -398,9 +398,9 @@ def test_blocks_of_every_size(dtype, store, dim, heads, group, page):
 
 
 @pytest.mark.parametrize("dtype,store", KINDS)
-@pytest.mark.parametrize("dim", [64, 128])
-def test_chunks_of_prompts(dtype, store, dim):
-    p = Paged(22, store, 1, dim, 16, [150, 2, 333], [150, 200, 400])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 8), (128, 256)])
+def test_chunks_of_prompts(dtype, store, dim, page):
+    p = Paged(22, store, 1, dim, page, [150, 2, 333], [150, 200, 400])
     attend(p, TYPES[dtype], 3)
 
 

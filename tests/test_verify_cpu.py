@@ -23,7 +23,7 @@ def _tokens(**kw):
 BAD_CACHES = [
     (dict(k=None), -1), (dict(v=None), -1), (dict(store=5), -1), (dict(store=-1), -1), (dict(store=api.COVSPEC_E4M3), -1),
     (dict(store=api.COVSPEC_INT8, k_scale=FAR), -1), (dict(head_dim=96), -3), (dict(head_dim=0), -3), (dict(page_size=24), -3),
-    (dict(page_size=0), -3), (dict(page_size=8192), -3), (dict(pages=0), -2), (dict(heads=0), -2),
+    (dict(page_size=0), -3), (dict(page_size=4), -3), (dict(page_size=8192), -3), (dict(pages=0), -2), (dict(heads=0), -2),
     (dict(k_page_stride=2 * 16 * 128 - 8), -2), (dict(v_page_stride=0), -2), (dict(k_page_stride=2 * 16 * 128 + 4), -1),
     (dict(k=FAR + 8), -1), (dict(heads=2 ** 20, page_size=4096), -2),
 ]
