@@ -94,19 +94,20 @@ struct Cursor {
   }
 };
 
-// Share `blockIdx.x` of gridDim.x: its first unit and the number of its units; every thread of the block calls it.
-// `scratch`: THREADS / 32 + 4 words of shared memory.
-template <int ROWS, int KEYS, int THREADS>
+// Share `blockIdx.x` of gridDim.x: its first unit and the number of its units; every thread of the block calls it.  Shares are cut from
+// a line on which an item is OPEN steps, what beginning and ending it costs, and then one for each unit; `first` and `per` are
+// places on it.  `scratch`: THREADS / 32 + 4 words of shared memory.
+template <int ROWS, int KEYS, int THREADS, int OPEN>
 __device__ __forceinline__ int find_share(const Params& p, Cursor<ROWS, KEYS>& c, long long& first, long long& per, long long* scratch) {
   long long* sums = scratch;
-  long long& place_unit = scratch[THREADS / 32];
+  long long& place_unit = scratch[THREADS / 32];       // units of the share
   int* place = reinterpret_cast<int*>(scratch + THREADS / 32 + 1);
   const int tid = threadIdx.x, each = (p.t.batch + THREADS - 1) / THREADS;
   const int b0 = min(tid * each, p.t.batch), b1 = min(b0 + each, p.t.batch);
   auto per_head = [&](const Request& r) {
     long long s = 0;
     const int tiles = (r.rows + ROWS - 1) / ROWS;
-    for (int t = 0; t < tiles; ++t) s += units_of<KEYS>(keys_of<ROWS>(p, r, t));
+    for (int t = 0; t < tiles; ++t) s += OPEN + units_of<KEYS>(keys_of<ROWS>(p, r, t));
     return s;
   };
   long long mine = 0;
@@ -128,8 +129,8 @@ __device__ __forceinline__ int find_share(const Params& p, Cursor<ROWS, KEYS>& c
   before += scan - mine;
   per = max((total + gridDim.x - 1) / gridDim.x, (long long)p.least_units);
   first = per * blockIdx.x;
-  const long long count = min(per, total - first);      // a share is far below 2^31 units: one is 64 keys at least
-  if (count <= 0) return 0;
+  const long long steps = min(per, total - first);
+  if (steps <= 0) return 0;
   if (first >= before && first < before + mine) {
     long long left = first - before;
     int b = b0;
@@ -145,14 +146,35 @@ __device__ __forceinline__ int find_share(const Params& p, Cursor<ROWS, KEYS>& c
     left -= h * u;
     int tile = 0;
     for (;; ++tile) {
-      const int n = units_of<KEYS>(keys_of<ROWS>(p, r, tile));
+      const int n = OPEN + units_of<KEYS>(keys_of<ROWS>(p, r, tile));
       if (left < n) break;
       left -= n;
+    }
+    const int unit = max((int)left - OPEN, 0);
+    long long count = steps;
+    if constexpr (OPEN > 0) {                             // the units among the steps; a share is far below 2^31 of them
+      Cursor<ROWS, KEYS> walk;
+      walk.b = b; walk.h = h; walk.tile = tile; walk.r = r;
+      walk.open(p);
+      count = 0;
+      for (long long todo = steps, at = left;;) {
+        const long long rest = OPEN + walk.units - at;
+        if (rest >= todo) {
+          count += max(at + todo - OPEN, 0ll) - max(at - OPEN, 0ll);
+          break;
+        }
+        count += walk.units - max(at - OPEN, 0ll);
+        todo -= rest;
+        at = 0;
+        walk.unit = walk.units - 1;
+        walk.next(p);
+      }
     }
     place[0] = b;
     place[1] = h;
     place[2] = tile;
-    place_unit = left;
+    place[3] = unit;
+    place_unit = count;
   }
   __syncthreads();
   c.b = place[0];
@@ -160,9 +182,9 @@ __device__ __forceinline__ int find_share(const Params& p, Cursor<ROWS, KEYS>& c
   c.tile = place[2];
   c.r = load_request(p, c.b);
   c.open(p);
-  c.unit = (int)place_unit;
+  c.unit = place[3];
   c.key += c.unit * KEYS;
-  return (int)count;
+  return (int)place_unit;
 }
 
 // Output row of tile row `row` of an item: element offset in a [tokens, q_heads, dim] array and the place in lse.

@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kThreads, (Layout<STORE, DIM, ROWS>::kCtas)) a
   Cursor<ROWS, kKeys> load;
   __shared__ long long scratch[kThreads / 32 + 4];
   long long first, per;
-  const int count = find_share<ROWS, kKeys, kThreads>(p, load, first, per, scratch);
+  const int count = find_share<ROWS, kKeys, kThreads, 0>(p, load, first, per, scratch);
   const int share = blockIdx.x;
   if (count <= 0) {
     if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);

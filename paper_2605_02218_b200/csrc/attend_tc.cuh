@@ -27,6 +27,7 @@ using namespace tc;
 constexpr int kRows = 256, kKeys = 128;
 constexpr int kThreads = 20 * 32, kSoftmaxWarps = 16;
 constexpr int kCopyWarps = 3, kProducers = kCopyWarps * 32;
+constexpr int kOpen = 4;                    // units that beginning and ending an item costs
 constexpr float kMost = 16384.f;            // a unit's probabilities add up to no more over their reference
 
 template <int STORE, int DIM> struct Layout {
@@ -180,7 +181,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   wait_for_previous_kernel();
   Cursor<kRows, kKeys> at;
   long long first, per;
-  const int count = find_share<kRows, kKeys, kThreads>(p, at, first, per, reinterpret_cast<long long*>(pages));
+  const int count = find_share<kRows, kKeys, kThreads, kOpen>(p, at, first, per, reinterpret_cast<long long*>(pages));
   const int share = blockIdx.x;
   if (count <= 0) {
     if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
@@ -238,18 +239,25 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     auto queries = [&] {                                       // of the item at `at`
       ok = ok && acquire(q_empty, q_phase);
       q_phase ^= 1u;
-      constexpr int kChunks = DIM / 8, kAtOnce = 32 / kChunks;
+      constexpr int kChunks = DIM / 8, kAtOnce = 32 / kChunks, kStep = kCopyWarps * kAtOnce;
       const int chunk = lane % kChunks;
+      // token and query head of row r, and how far they go on from one of this thread's rows to the next
+      int row = wp * kAtOnce + lane / kChunks;
+      int token = (at.tile * kRows + row) / p.group, head = at.tile * kRows + row - token * p.group;
+      const int step_token = kStep / p.group, step_head = kStep - step_token * p.group, rows = ok ? at.r.rows - at.tile * kRows : 0;
+      const T* q0 = static_cast<const T*>(p.q) + at.r.q0 * p.q_ld + (long long)at.h * p.group * DIM + chunk * 8;
 #pragma unroll 4
-      for (int row0 = wp * kAtOnce; row0 < kRows; row0 += kCopyWarps * kAtOnce) {
-        const int row = row0 + lane / kChunks, r = at.tile * kRows + row;
-        const bool in = row < kRows, is = ok && in && r < at.r.rows;
-        const T* q = static_cast<const T*>(p.q) + (is ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM + chunk * 8 : 0);
+      for (int i = 0; i < (kRows + kStep - 1) / kStep; ++i, row += kStep) {
+        const bool in = row < kRows, is = row < min(rows, kRows);
+        const T* q = is ? q0 + token * p.q_ld + head * DIM : q0;
+        token += step_token;
+        head += step_head;
+        if (head >= p.group) { head -= p.group; ++token; }
         uint8_t* to = smem + (row >> 7) * (128 * DIM * 2) + tile_at(128, row & 127, chunk);
         if constexpr (!kConvert) {
           if (in) copy16(smem_u32(to), q, is);
         } else {
-          uint4 w = is ? *reinterpret_cast<const uint4*>(q) : make_uint4(0u, 0u, 0u, 0u);
+          const uint4 w = is ? *reinterpret_cast<const uint4*>(q) : make_uint4(0u, 0u, 0u, 0u);
           float most = largest_of(w.x, largest_of(w.y, largest_of(w.z, largest_of(w.w, 0.f))));
 #pragma unroll
           for (int o = kChunks / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
@@ -727,7 +735,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         if (u + 1 == count && tid == 0) {
           const bool open = !(flags & kEnds) && (flags & kWholeStart);
           p.open[2 * share] = make_int4(q0, h, item.x, min(kRows, item.y - item.x));
-          p.open[2 * share + 1] = make_int4(open ? (int)((first + u + item.w) / per) : -1, 0, 0, 0);
+          p.open[2 * share + 1] = make_int4(open ? (int)((first + per + item.w - 1) / per) : -1, 0, 0, 0);
         }
       }
     }
