@@ -241,7 +241,7 @@ typedef struct {
   int head_dim;                /* 64 or 128                                                        */
   void* k;
   void* v;
-  float* k_scale;              /* 8-bit stores only                                                */
+  float* k_scale;              /* 8-bit stores only; 16-byte aligned                               */
   float* v_scale;
   long long k_page_stride, v_page_stride;
 } covspec_cache;

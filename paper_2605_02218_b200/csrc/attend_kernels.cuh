@@ -1,7 +1,11 @@
 // Attention of few rows per key head (single tokens, drafted blocks) over the paged cache: one pass over the keys with running
-// maxima and sums.  A tile is 16, 32 or 64 rows (16 a warp; warps left over share the keys of a unit) and 64 keys, with 8-bit rows and 16-row tiles 128.  The work is
-// bound by reading the cache, so operands go to the tensor cores through registers (mma.sync): shared memory holds the pages'
-// rows as they are in the cache, 8-bit ones are widened in registers.
+// maxima and sums.  A tile is 16, 32 or 64 rows (16 a warp; the warps left of four share the keys of a unit) and 64 keys, 128 with
+// 8-bit rows and up to 32 rows of queries.  The work is bound by reading the cache, so operands go to the tensor cores through
+// registers (mma.sync): shared memory holds the pages' rows as they are in the cache, 8-bit ones are widened in registers.
+//
+// Warp 4 loads: tiled copies, a box as many rows of one head as a page has (at most a unit's), a box a lane, into a ring of units;
+// it tells the others what each unit is, and where not every key is there it clears the values of the rest.  The others go from
+// unit to unit each at its own pace and meet at the end of an item only.
 //
 // 8-bit rows are exact in float16, so their scales stay outside the products: s_ij = (q_i . k_j) * key scale, and the probability
 // takes the value's scale before it is rounded to 16 bits.  So that it cannot leave float16's range, the running maximum is the
@@ -14,36 +18,37 @@
 namespace covspec {
 namespace attend {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 160, kWarps = 4;        // threads of a CTA; its warps that compute
 
 template <int STORE, int DIM, int ROWS> struct Layout {
   static constexpr bool k8 = STORE >= cache::kE4M3;
-  static constexpr int kKeys = k8 && ROWS == 16 ? 128 : 64;    // of a unit
+  static constexpr int kKeys = k8 && ROWS < 64 ? 128 : 64;     // of a unit
   static constexpr int kCtas = 2;                              // on an SM
   static constexpr int kRow = DIM * (k8 ? 1 : 2);              // bytes of a key's row
   static constexpr int kChunks = kRow / 16;
-  static constexpr int kStage = 2 * kKeys * kRow;              // keys, values
-  static constexpr int kScale = k8 ? 2 * kKeys * 4 : 0;        // per stage: the keys' and the values' scales
-  static constexpr int kFixed = 2 * 2 * kKeys * 4 + 8 * 16 + 2 * 16 * 8 + 128;   // places of two units; keys there; maxima and sums of two warps' rows
-  static constexpr int kFit = (233472 / kCtas - 1024 - 128 - kFixed) / (kStage + kScale);   // an SM's shared memory, 1 KB of it a CTA's own
+  static constexpr int kBlock = kRow < 128 ? kRow : 128;       // bytes of a row in a box; a row of 256 bytes has two
+  static constexpr int kBoxes = 16 / (kRow / kBlock);          // of a unit at most: 16 lanes copy keys, 16 values
+  static constexpr int kTile = kKeys * kRow;                   // keys, or values
+  static constexpr int kScales = k8 ? 2 * kKeys * 4 : 0;       // the keys' and the values'
+  static constexpr int kSay = 48;                              // what a unit is, which keys are there
+  static constexpr int kStage = 2 * kTile;
+  static constexpr int kFixed = 1024 + 256 + 2 * 16 * 8;       // alignment; barriers; maxima and sums of two warps' rows
+  static constexpr int kFit = (233472 / kCtas - 1024 - 256 - kFixed) / (kStage + kScales + kSay);   // an SM's shared memory, 1 KB of it a CTA's own
   static constexpr int kStages = kFit < 6 ? kFit : 6;
-  static constexpr int kSmem = kStages * (kStage + kScale) + kFixed;
-  static_assert(kStages >= 2 && (ROWS == 64 || kStage >= 2 * 16 * DIM * 4));
+  static constexpr int kSmem = kStages * (kStage + kScales + kSay) + kFixed;
+  static_assert(kStages >= 2 && kKeys / 8 <= kBoxes && (ROWS == 64 || kStage >= 2 * 16 * DIM * 4));
 };
-// Byte offset of a 16-byte chunk of a row: chunks are permuted so that eight rows' chunks of one column lie in different banks.
-template <int ROW> __device__ __forceinline__ int swizzled(int row, int chunk) {
-  if constexpr (ROW >= 128) return row * ROW + ((chunk ^ (row & 7)) << 4);
+// Byte offset of a 16-byte chunk of a row as the tiled copies leave it: chunks are permuted so that eight rows' chunks of one column
+// lie in different banks.
+template <int ROW, int KEYS> __device__ __forceinline__ int swizzled(int row, int chunk) {
+  if constexpr (ROW >= 128) return (chunk >> 3) * (KEYS * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
   else return row * ROW + ((chunk ^ ((row >> 1) & 3)) << 4);
 }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
-}
 __device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-constexpr uint32_t kNowhere = 0xffffffffu;
 __device__ __forceinline__ float ex2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -111,360 +116,426 @@ __device__ __forceinline__ float largest_of(uint32_t two, float top) {
   return fmaxf(top, fmaxf(fabsf(__uint_as_float(two << 16)), fabsf(__uint_as_float(two & 0xffff0000u))));
 }
 
+// What the loading warp tells the others of a unit: {first key, flags, first token of the request, head}, {first row of the item, rows of
+// the request, position of its first token, units of the item behind this one}, which keys are there.
+constexpr int kBegins = 1, kEnds = 2, kTwo = 4, kWholeStart = 8;   // first unit of its item in this share; last one of the item; more than
+                                                                   // 128 rows; the item's first unit is in this share
+
+__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(tc::smem_u32(bar))
+      : "memory");
+}
+// A multiple of 16 bytes between 16-byte aligned addresses.
+__device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(tc::smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 template <typename T, int STORE, int DIM, int ROWS>
-__global__ void __launch_bounds__(kThreads, (Layout<STORE, DIM, ROWS>::kCtas)) attend_kernel(Params p) {
+__global__ void __launch_bounds__(kThreads, (Layout<STORE, DIM, ROWS>::kCtas))
+attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p) {
+  using namespace tc;
   using L = Layout<STORE, DIM, ROWS>;
   constexpr bool k8 = L::k8;
   using M = std::conditional_t<k8, __half, T>;                 // type of the products
-  constexpr int kKeys = L::kKeys, kWords = kKeys / 32;
-  constexpr int kWarpsM = ROWS / 16, kWarpsK = 4 / kWarpsM;    // warps along the rows, along the keys of a unit
+  constexpr int kKeys = L::kKeys;
+  constexpr int kWarpsM = ROWS / 16, kWarpsK = kWarps / kWarpsM;   // warps along the rows, along the keys of a unit
   constexpr int kMine = kKeys / kWarpsK;                       // keys of a unit that one warp takes
   constexpr int kS = L::kStages;
   extern __shared__ char smem_raw[];
-  char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~(uintptr_t)127);
-  float* scales = reinterpret_cast<float*>(smem + kS * L::kStage);
-  uint32_t* places = reinterpret_cast<uint32_t*>(scales + kS * (L::kScale / 4));   // [2][2][kKeys]: keys', values' rows in 16 bytes
-  float2* box_ts = reinterpret_cast<float2*>(places + 4 * kKeys);                  // [2][16]
-  uint32_t* there = reinterpret_cast<uint32_t*>(box_ts + 2 * 16);                  // [kS + 1][kWords]: which keys of a unit are there
-  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
-  const int wm = warp / kWarpsK, wk = warp % kWarpsK;
-  const int g = lane >> 2, tq = lane & 3;
-
-  wait_for_previous_kernel();
-  Cursor<ROWS, kKeys> load;
+  char* smem = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
+  char* says = smem + kS * (L::kStage + L::kScales);           // [kS][kSay]
+  float2* box_ts = reinterpret_cast<float2*>(says + kS * L::kSay);   // [2][16]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(box_ts + 2 * 16);
+  uint64_t *full = bars, *empty = bars + 6, *partly = bars + 12, *met = bars + 13;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 14);
   __shared__ long long scratch[kThreads / 32 + 4];
-  long long first, per;
-  const int count = find_share<ROWS, kKeys, kThreads, 0>(p, load, first, per, scratch);
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < kS; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, kWarps); }
+    mbar_init(partly, 1);
+    mbar_init(met, kWarps);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  wait_for_previous_kernel();
   const int share = blockIdx.x;
+  Cursor<ROWS, kKeys> at;
+  long long first, per;
+  const int count = find_share<ROWS, kKeys, kThreads, 0>(p, at, first, per, scratch);
+  if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
   if (count <= 0) {
-    if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
     launch_dependents_now();
     return;
   }
-  Cursor<ROWS, kKeys> at = load;
+  __syncthreads();
 
-  // ---- copies of one unit: keys and values of 64 positions, zeros where there is none.  The places of its keys, one a thread, are
-  // worked out an iteration before, and the pages are fetched one before that ----
-  constexpr int kRowsPerPass = kThreads / L::kChunks;
-  const int ld_chunk = tid % L::kChunks, ld_row = tid / L::kChunks;
-  int page = -1, issued = 0, word = 0;          // page of key `tid` of the unit at `load`; units copied; unit modulo kS + 1
-  [[maybe_unused]] long long scale_at = -1;
-  auto look_up = [&] {
-    const int key = load.key + tid;
-    if (tid < kKeys) page = key >= load.k.lo && key < load.k.hi ? p.t.table[load.b * p.t.table_ld + (key >> p.c.page_shift)] : -1;
-  };
-  auto publish = [&] {
-    if (tid < kKeys && issued < count) {
-      const bool ok = (unsigned)page < (unsigned)p.c.pages;
-      const int in = (load.h << p.c.page_shift) + ((load.key + tid) & ((1 << p.c.page_shift) - 1));
-      uint32_t* place = places + (issued & 1) * 2 * kKeys + tid;
-      auto row = [&](long long page_ld) { return (uint32_t)((unsigned long long)(page * page_ld + (long long)in * DIM) / (16 / (L::kRow / DIM))); };
-      place[0] = ok ? row(p.c.k_page) : kNowhere;
-      place[kKeys] = ok ? row(p.c.v_page) : kNowhere;
-      const uint32_t bits = __ballot_sync(0xffffffffu, ok);
-      if (lane == 0) there[kWords * word + warp] = bits;
-      if constexpr (k8) scale_at = ok ? (((long long)page * p.c.heads) << p.c.page_shift) + in : -1;
-    }
-    word = word == kS ? 0 : word + 1;
-  };
-  auto copy_unit = [&](int stage) {
-    if (issued < count) {
-      char* base = smem + stage * L::kStage;
-      const uint32_t* place = places + (issued & 1) * 2 * kKeys;
-      constexpr int kPer = kKeys / kRowsPerPass;
-      uint32_t at[kPer][2];
+  if (warp == kWarps) {
+    // ---------------- the loading warp ----------------
+    const int mask = (1 << p.c.page_shift) - 1, shift = min(p.c.page_shift, kKeys == 128 ? 7 : 6), rows = 1 << shift, boxes = kKeys >> shift;
+    const int kv = lane >> 4, box = lane & (L::kBoxes - 1), part = (lane & 15) / L::kBoxes;   // this lane's box of a unit
+    int page = -1, stage = 0;
+    auto look_up = [&] {                                       // its page in the unit at `at`
+      const int key = at.key + (box << shift);
+      page = box < boxes && key < at.k.hi && key + rows > at.k.lo ? p.t.table[at.b * p.t.table_ld + (key >> p.c.page_shift)] : -1;
+      if ((unsigned)page >= (unsigned)p.c.pages) page = -1;
+    };
+    bool fresh = true, whole_start = false, ok = true;
+    uint32_t phase = 1, part_phase = 0;
+    look_up();
+    for (int u = 0; u < count; ++u) {
+      if (fresh) whole_start = at.unit == 0;
+      const int key0 = at.key, row0 = at.tile * ROWS;
+      const bool ends = at.unit + 1 == at.units;
+      const int4 say0 = make_int4(key0, (fresh ? kBegins : 0) | (ends ? kEnds : 0) | (whole_start ? kWholeStart : 0), at.r.q0, at.h);
+      const int4 say1 = make_int4(row0, at.r.rows, at.r.length - at.r.n, at.units - 1 - at.unit);
+      fresh = ends;
+      const int page_row = (at.h << p.c.page_shift) + ((key0 + (box << shift)) & mask), box_page = page;
+      uint32_t word[kKeys / 32], all = 0xffffffffu;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        at[i][0] = place[i * kRowsPerPass + ld_row];
-        at[i][1] = place[kKeys + i * kRowsPerPass + ld_row];
+      for (int i = 0; i < kKeys / 32; ++i) {
+        const int j = 32 * i + lane, has = __shfl_sync(0xffffffffu, page, j >> shift);
+        word[i] = __ballot_sync(0xffffffffu, has >= 0 && key0 + j >= at.k.lo && key0 + j < at.k.hi);
+        all &= word[i];
       }
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int off = swizzled<L::kRow>(i * kRowsPerPass + ld_row, ld_chunk);
-        const bool ok = at[i][0] != kNowhere;
-        copy16(tc::smem_u32(base + off), static_cast<const char*>(p.c.k) + (ok ? (unsigned long long)at[i][0] * 16 + ld_chunk * 16 : 0ull), ok);
-        copy16(tc::smem_u32(base + kKeys * L::kRow + off), static_cast<const char*>(p.c.v) + (ok ? (unsigned long long)at[i][1] * 16 + ld_chunk * 16 : 0ull), ok);
-      }
-      if constexpr (k8) {
-        if (tid < kKeys) {
-          float* s = scales + stage * 2 * kKeys + tid;
-          copy4(tc::smem_u32(s), p.c.k_scale + (scale_at >= 0 ? scale_at : 0), scale_at >= 0);
-          copy4(tc::smem_u32(s + kKeys), p.c.v_scale + (scale_at >= 0 ? scale_at : 0), scale_at >= 0);
-        }
-      }
-      if (++issued < count) {
-        load.next(p);
+      const bool mine = page >= 0;
+      constexpr int kScaleBytes = k8 ? 4 : 0;
+      // the first part's lane brings a box's scales too
+      const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * rows * (L::kBlock + kScaleBytes);
+      if (u + 1 < count) {
+        at.next(p);
         look_up();
       }
-    }
-    copies_close();
-  };
-  look_up();
-  for (int s = 0; s < kS - 1; ++s) {
-    publish();
-    __syncthreads();
-    copy_unit(s);
-  }
-
-  uint32_t qf[DIM / 16][4];
-  float o[DIM / 8][4], top[2], sum[2];
-  int pos[2];                     // position of the thread's two rows; -1 where there is no row
-  [[maybe_unused]] float row_scale[2] = {p.scale_log2, p.scale_log2};
-  int low = 0, high = 0;          // the lowest of them, the highest before the highest one's window
-  int began = 0;                  // the item's first unit, counted from the share's
-  bool fresh = true;
-  int stage = 0, seen = 0;        // stage and word of unit u
-  for (int u = 0; u < count; ++u) {
-    if (fresh) {                  // a new item: its query rows
-      fresh = false;
-      began = u - at.unit;
-      low = 0x7fffffff;
-      high = -0x7fffffff;
-      const int r0 = at.tile * ROWS + wm * 16 + g;
+      if (!(ok = mbar_wait(empty + stage, phase, abort_flag))) break;
+      char* base = smem + stage * L::kStage;
+      float* sc = reinterpret_cast<float*>(smem + kS * L::kStage) + stage * 2 * kKeys;
+      uint64_t* bar = all == 0xffffffffu ? full + stage : partly;
+      if (lane == 0) {
+        int4* say = reinterpret_cast<int4*>(says + stage * L::kSay);
+        say[0] = say0;
+        say[1] = say1;
+        uint32_t* there = reinterpret_cast<uint32_t*>(say + 2);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = r0 + 8 * i;
-        const bool ok = r < at.r.rows;
-        pos[i] = ok ? at.r.length - at.r.n + r / p.group : -1;
-        if (ok) {
-          low = min(low, pos[i]);
-          high = max(high, pos[i] - p.window);
-        }
-        const T* q = static_cast<const T*>(p.q) + (ok ? token_of(p, at.r.q0, r) * p.q_ld + (long long)head_of(p, at.h, r) * DIM : 0);
-#pragma unroll
-        for (int s = 0; s < DIM / 16; ++s) {
-          // the order of the products' inner index is free: 8-bit keys come as four neighbours a thread
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(q + 16 * s);
-          qf[s][i] = ok ? w[k8 ? 2 * tq : tq] : 0u;
-          qf[s][2 + i] = ok ? w[k8 ? 2 * tq + 1 : tq + 4] : 0u;
-        }
-        if constexpr (!__is_same(M, T)) {
-          float most = 0.f;
-#pragma unroll
-          for (int s = 0; s < DIM / 16; ++s) most = largest_of(qf[s][2 + i], largest_of(qf[s][i], most));
-          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-          const float f = power_for(most);
-#pragma unroll
-          for (int s = 0; s < DIM / 16; ++s) { qf[s][i] = to_half(qf[s][i], f); qf[s][2 + i] = to_half(qf[s][2 + i], f); }
-          row_scale[i] = p.scale_log2 * inverse_power(f);
-        }
-        top[i] = -INFINITY;
-        sum[i] = 0.f;
+        for (int i = 0; i < kKeys / 32; ++i) there[i] = word[i];
+        mbar_expect_tx(bar, bytes);
       }
+      __syncwarp();
+      if (mine) {
+        tma_load_3d(smem_u32(base + kv * L::kTile + part * (kKeys * 128) + (box << shift) * L::kBlock), kv ? &map_v : &map_k,
+                    part * (L::kBlock / (L::kRow / DIM)), page_row, box_page, bar);
+        if constexpr (k8)
+          bulk_load(smem_u32(sc + kv * kKeys + (box << shift)), (kv ? p.c.v_scale : p.c.k_scale) + ((((long long)box_page * p.c.heads) << p.c.page_shift) + page_row),
+                    rows * 4, bar);
+      }
+      if (all != 0xffffffffu) {                                // values of keys that are not there: zeros, whatever memory holds
+        if (!(ok = mbar_wait(partly, part_phase, abort_flag))) break;
+        part_phase ^= 1u;
 #pragma unroll
-      for (int j = 0; j < DIM / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+        for (int i = 0; i < kKeys / 32; ++i)
+          if (!((word[i] >> lane) & 1u)) {
+            for (int c = 0; c < L::kChunks; ++c)
+              *reinterpret_cast<uint4*>(base + L::kTile + swizzled<L::kRow, kKeys>(32 * i + lane, c)) = make_uint4(0u, 0u, 0u, 0u);
+            if constexpr (k8) sc[kKeys + 32 * i + lane] = 0.f;
+          }
+        fence_async_proxy();                                   // before copies into the same place
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full + stage);
+      }
+      if (++stage == kS) { stage = 0; phase ^= 1u; }
     }
-    copies_wait<kS - 2>();
-    publish();
-    __syncthreads();
-    copy_unit(stage == 0 ? kS - 1 : stage - 1);
-    // ---- scores of this warp's keys ----
-    const char* kbase = smem + stage * L::kStage;
-    const char* vbase = kbase + kKeys * L::kRow;
-    float s[kMine / 8][4];
+    // copies under way end before their memory goes, also after a wait that gave up
+    for (int i = 0; i < kS && !ok; ++i) {
+      volatile int gave_up = 0;
+      mbar_wait_limited(full + i, 0, &gave_up, 1u << 16);
+      mbar_wait_limited(full + i, 1, &gave_up, 1u << 16);
+    }
+  } else {
+    // ---------------- the computing warps ----------------
+    const int wm = warp / kWarpsK, wk = warp % kWarpsK;
+    const int g = lane >> 2, tq = lane & 3;
+    uint32_t qf[DIM / 16][4];
+    float o[DIM / 8][4], top[2], sum[2];
+    int pos[2] = {-1, -1};        // position of the thread's two rows; -1 where there is no row
+    [[maybe_unused]] float row_scale[2] = {p.scale_log2, p.scale_log2};
+    int low = 0, high = 0;        // the lowest of them, the highest before the highest one's window
+    int stage = 0;
+    uint32_t phase = 0, met_phase = 0;
+    bool ok = true, inside = false;   // between an item's first unit and its last
+    int q0 = 0, h = 0, tile_row = 0;  // the item at hand
+    auto meet = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(met);
+      ok = mbar_wait(met, met_phase, abort_flag) && ok;
+      met_phase ^= 1u;
+    };
+    for (int u = 0; u < count; ++u) {
+      if (!(ok = mbar_wait(full + stage, phase, abort_flag) && ok)) break;
+      const int4* say = reinterpret_cast<const int4*>(says + stage * L::kSay);
+      const uint32_t* there = reinterpret_cast<const uint32_t*>(say + 2);
+      const int flags = say[0].y;
+      if (flags & kBegins) {
+        const int4 a = say[0], b = say[1];
+        inside = true;
+        q0 = a.z;
+        h = a.w;
+        tile_row = b.x;
+        low = 0x7fffffff;
+        high = -0x7fffffff;
 #pragma unroll
-    for (int j = 0; j < kMine / 8; ++j) {
-      s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-      const int row = wk * kMine + j * 8 + (lane & 7);
+        for (int i = 0; i < 2; ++i) {
+          const int r = tile_row + wm * 16 + g + 8 * i;
+          const bool is = r < b.y;
+          const int token = r / p.group;
+          pos[i] = is ? b.z + token : -1;
+          if (is) {
+            low = min(low, pos[i]);
+            high = max(high, pos[i] - p.window);
+          }
+          const T* q = static_cast<const T*>(p.q) + (is ? (long long)(q0 + token) * p.q_ld + (long long)(h * p.group + r - token * p.group) * DIM : 0);
 #pragma unroll
-      for (int c = 0; c < L::kChunks; c += 4) {
-        uint32_t kf[4];
-        ldm4(kf, tc::smem_u32(kbase + swizzled<L::kRow>(row, c + (lane >> 3))));
+          for (int s = 0; s < DIM / 16; ++s) {
+            // the order of the products' inner index is free: 8-bit keys come as four neighbours a thread
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(q + 16 * s);
+            qf[s][i] = is ? w[k8 ? 2 * tq : tq] : 0u;
+            qf[s][2 + i] = is ? w[k8 ? 2 * tq + 1 : tq + 4] : 0u;
+          }
+          if constexpr (!__is_same(M, T)) {
+            float most = 0.f;
+#pragma unroll
+            for (int s = 0; s < DIM / 16; ++s) most = largest_of(qf[s][2 + i], largest_of(qf[s][i], most));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const float f = power_for(most);
+#pragma unroll
+            for (int s = 0; s < DIM / 16; ++s) { qf[s][i] = to_half(qf[s][i], f); qf[s][2 + i] = to_half(qf[s][2 + i], f); }
+            row_scale[i] = p.scale_log2 * inverse_power(f);
+          }
+          top[i] = -INFINITY;
+          sum[i] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < DIM / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+      }
+      // ---- scores of this warp's keys ----
+      const char* kbase = smem + stage * L::kStage;
+      const char* vbase = kbase + L::kTile;
+      float s[kMine / 8][4];
+#pragma unroll
+      for (int j = 0; j < kMine / 8; ++j) {
+        s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+        const int row = wk * kMine + j * 8 + (lane & 7);
+#pragma unroll
+        for (int c = 0; c < L::kChunks; c += 4) {
+          uint32_t kf[4];
+          ldm4(kf, smem_u32(kbase + swizzled<L::kRow, kKeys>(row, c + (lane >> 3))));
+          if constexpr (k8) {
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {                    // every other chunk by conversions: both units are kept busy
+              mma<M>(s[j], qf[c + i], widen<STORE, true>(kf[i], 0, 1), widen<STORE, true>(kf[i], 2, 3));
+              mma<M>(s[j], qf[c + i + 1], widen<STORE, false>(kf[i + 1], 0, 1), widen<STORE, false>(kf[i + 1], 2, 3));
+            }
+          } else {
+            mma<M>(s[j], qf[c / 2], kf[0], kf[1]);
+            mma<M>(s[j], qf[c / 2 + 1], kf[2], kf[3]);
+          }
+        }
+      }
+      // ---- running maxima and sums ----
+      const float* sc = reinterpret_cast<const float*>(smem + kS * L::kStage) + stage * 2 * kKeys + wk * kMine;
+      uint64_t see_all;                                          // of this warp's keys
+      if constexpr (kMine == 64) see_all = *reinterpret_cast<const uint64_t*>(there + wk * 2);
+      else see_all = there[wk * kMine / 32] >> (wk * kMine % 32);
+      const int key0 = say[0].x + wk * kMine;
+      // every row of the warp sees all of its keys
+      const bool clear = (kMine == 64 ? see_all == ~0ull : (see_all & ((1ull << (kMine & 63)) - 1)) == (1ull << (kMine & 63)) - 1) &&
+                         __all_sync(0xffffffffu, key0 + kMine - 1 <= low && (p.window == 0 || key0 > high));
+      float best[2] = {top[0], top[1]};
+#pragma unroll
+      for (int j = 0; j < kMine / 8; ++j) {
+        [[maybe_unused]] float by[2], lift[2];
         if constexpr (k8) {
 #pragma unroll
-          for (int i = 0; i < 4; i += 2) {                      // every other chunk by conversions: both units are kept busy
-            mma<M>(s[j], qf[c + i], widen<STORE, true>(kf[i], 0, 1), widen<STORE, true>(kf[i], 2, 3));
-            mma<M>(s[j], qf[c + i + 1], widen<STORE, false>(kf[i + 1], 0, 1), widen<STORE, false>(kf[i + 1], 2, 3));
-          }
-        } else {
-          mma<M>(s[j], qf[c / 2], kf[0], kf[1]);
-          mma<M>(s[j], qf[c / 2 + 1], kf[2], kf[3]);
-        }
-      }
-    }
-    // ---- running maxima and sums ----
-    const float* sc = scales + stage * 2 * kKeys + wk * kMine;
-    uint64_t see_all;                                          // of this warp's keys
-    if constexpr (kMine == 64) see_all = (uint64_t)there[kWords * seen + 1] << 32 | there[kWords * seen];
-    else see_all = there[kWords * seen + wk * kMine / 32] >> (wk * kMine % 32);
-    const int key0 = at.key + wk * kMine;
-    // every row of the warp sees all of its keys
-    const bool clear = (kMine == 64 ? see_all == ~0ull : (see_all & ((1ull << (kMine & 63)) - 1)) == (1ull << (kMine & 63)) - 1) &&
-                       __all_sync(0xffffffffu, key0 + kMine - 1 <= low && (p.window == 0 || key0 > high));
-    float best[2] = {top[0], top[1]};
-#pragma unroll
-    for (int j = 0; j < kMine / 8; ++j) {
-      [[maybe_unused]] float by[2], lift[2];
-      if constexpr (k8) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          by[i] = sc[j * 8 + 2 * tq + i];
-          lift[i] = exponent_of(sc[kKeys + j * 8 + 2 * tq + i]);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int col = j * 8 + 2 * tq + (e & 1), i = e >> 1;
-        s[j][e] *= k8 ? by[e & 1] * row_scale[i] : p.scale_log2;
-        if (!clear) {
-          const int key = key0 + col;
-          const bool see = (see_all >> col) & 1u && key <= pos[i] && (p.window == 0 || key > pos[i] - p.window);
-          s[j][e] = see ? s[j][e] : -INFINITY;
-        }
-        best[i] = fmaxf(best[i], k8 ? s[j][e] + lift[e & 1] : s[j][e]);
-      }
-    }
-    float safe[2], shrink[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 1));
-      best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 2));
-      safe[i] = best[i] == -INFINITY ? 0.f : best[i];
-      shrink[i] = ex2(top[i] - safe[i]);
-      top[i] = best[i];
-      sum[i] *= shrink[i];
-    }
-    if (__any_sync(0xffffffffu, shrink[0] != 1.f || shrink[1] != 1.f)) {
-#pragma unroll
-      for (int j = 0; j < DIM / 8; ++j) { o[j][0] *= shrink[0]; o[j][1] *= shrink[0]; o[j][2] *= shrink[1]; o[j][3] *= shrink[1]; }
-    }
-    uint32_t pf[kMine / 16][4];
-#pragma unroll
-    for (int j = 0; j < kMine / 8; ++j) {
-      float e[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        e[x] = ex2(s[j][x] - safe[x >> 1]);
-        sum[x >> 1] += e[x];
-        if constexpr (k8) e[x] *= sc[kKeys + j * 8 + 2 * tq + (x & 1)];
-      }
-      pf[j / 2][(j & 1) * 2] = pack2of<M>(e[0], e[1]);
-      pf[j / 2][(j & 1) * 2 + 1] = pack2of<M>(e[2], e[3]);
-    }
-    // ---- values ----
-#pragma unroll
-    for (int s16 = 0; s16 < kMine / 16; ++s16) {
-      const int row0 = wk * kMine + s16 * 16;
-      if constexpr (k8) {
-#pragma unroll
-        for (int c = 0; c < L::kChunks; c += 2) {              // 32 features: chunks c, c + 1 of the 16 keys
-          uint32_t vf[4];                                      // [chunk][keys 0-7, 8-15]
-          ldm4t(vf, tc::smem_u32(vbase + swizzled<L::kRow>(row0 + (lane & 15), c + (lane >> 4))));
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            // a register holds features 2n, 2n + 1 of two keys: the even ones make one tile of eight columns, the odd ones another
-            mma<M>(o[2 * (c + h)], pf[s16], widen<STORE, false>(vf[2 * h], 0, 2), widen<STORE, false>(vf[2 * h + 1], 0, 2));
-            mma<M>(o[2 * (c + h) + 1], pf[s16], widen<STORE, false>(vf[2 * h], 1, 3), widen<STORE, false>(vf[2 * h + 1], 1, 3));
+          for (int i = 0; i < 2; ++i) {
+            by[i] = sc[j * 8 + 2 * tq + i];
+            lift[i] = exponent_of(sc[kKeys + j * 8 + 2 * tq + i]);
           }
         }
-      } else {
 #pragma unroll
-        for (int c = 0; c < L::kChunks; c += 2) {
-          uint32_t vf[4];
-          ldm4t(vf, tc::smem_u32(vbase + swizzled<L::kRow>(row0 + (lane & 15), c + (lane >> 4))));
-          mma<M>(o[c], pf[s16], vf[0], vf[1]);
-          mma<M>(o[c + 1], pf[s16], vf[2], vf[3]);
+        for (int e = 0; e < 4; ++e) {
+          const int col = j * 8 + 2 * tq + (e & 1), i = e >> 1;
+          s[j][e] *= k8 ? by[e & 1] * row_scale[i] : p.scale_log2;
+          if (!clear) {
+            const int key = key0 + col;
+            const bool see = (see_all >> col) & 1u && key <= pos[i] && (p.window == 0 || key > pos[i] - p.window);
+            s[j][e] = see ? s[j][e] : -INFINITY;
+          }
+          best[i] = fmaxf(best[i], k8 ? s[j][e] + lift[e & 1] : s[j][e]);
         }
       }
-    }
-
-    // ---- the item's end, or the share's ----
-    const bool last = at.unit + 1 == at.units;
-    if (last || u + 1 == count) {
+      float safe[2], shrink[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
-        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+        best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 1));
+        best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 2));
+        safe[i] = best[i] == -INFINITY ? 0.f : best[i];
+        shrink[i] = ex2(top[i] - safe[i]);
+        top[i] = best[i];
+        sum[i] *= shrink[i];
       }
-      // warps that shared the keys: the upper half hands its rows to the lower one, until one has all; through the unit's own
-      // stage, which takes no copies before the next barrier
+      if (__any_sync(0xffffffffu, shrink[0] != 1.f || shrink[1] != 1.f)) {
 #pragma unroll
-      for (int half = kWarpsK / 2; half > 0; half >>= 1) {
-        __syncthreads();
-        const int which = kWarpsK == 4 ? (wk & (half - 1)) : wm;
-        float* box = reinterpret_cast<float*>(smem + stage * L::kStage) + which * 16 * DIM;
-        if (wk >= half && wk < 2 * half) {
+        for (int j = 0; j < DIM / 8; ++j) { o[j][0] *= shrink[0]; o[j][1] *= shrink[0]; o[j][2] *= shrink[1]; o[j][3] *= shrink[1]; }
+      }
+      uint32_t pf[kMine / 16][4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float* x = box + (g + 8 * i) * DIM;
+      for (int j = 0; j < kMine / 8; ++j) {
+        float e[4];
 #pragma unroll
-            for (int j = 0; j < DIM / 8; ++j) *reinterpret_cast<float2*>(x + ((j ^ g) * 8 + 2 * tq)) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
-            if (tq == 0) box_ts[which * 16 + g + 8 * i] = make_float2(top[i], sum[i]);
-          }
+        for (int x = 0; x < 4; ++x) {
+          e[x] = ex2(s[j][x] - safe[x >> 1]);
+          sum[x >> 1] += e[x];
+          if constexpr (k8) e[x] *= sc[kKeys + j * 8 + 2 * tq + (x & 1)];
         }
-        __syncthreads();
-        if (wk < half) {
+        pf[j / 2][(j & 1) * 2] = pack2of<M>(e[0], e[1]);
+        pf[j / 2][(j & 1) * 2 + 1] = pack2of<M>(e[2], e[3]);
+      }
+      // ---- values ----
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float* x = box + (g + 8 * i) * DIM;
-            const float2 ts = box_ts[which * 16 + g + 8 * i];
-            const float both = fmaxf(top[i], ts.x), ref = both == -INFINITY ? 0.f : both;
-            const float a = ex2(top[i] - ref), b = ex2(ts.x - ref);
-            top[i] = both;
-            sum[i] = sum[i] * a + ts.y * b;
+      for (int s16 = 0; s16 < kMine / 16; ++s16) {
+        const int row0 = wk * kMine + s16 * 16;
+        if constexpr (k8) {
 #pragma unroll
-            for (int j = 0; j < DIM / 8; ++j) {
-              const float2 v = *reinterpret_cast<const float2*>(x + ((j ^ g) * 8 + 2 * tq));
-              o[j][2 * i] = o[j][2 * i] * a + v.x * b;
-              o[j][2 * i + 1] = o[j][2 * i + 1] * a + v.y * b;
+          for (int c = 0; c < L::kChunks; c += 2) {              // 32 features: chunks c, c + 1 of the 16 keys
+            uint32_t vf[4];                                      // [chunk][keys 0-7, 8-15]
+            ldm4t(vf, tc::smem_u32(vbase + swizzled<L::kRow, kKeys>(row0 + (lane & 15), c + (lane >> 4))));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              // a register holds features 2n, 2n + 1 of two keys: the even ones make one tile of eight columns, the odd ones another
+              mma<M>(o[2 * (c + h)], pf[s16], widen<STORE, false>(vf[2 * h], 0, 2), widen<STORE, false>(vf[2 * h + 1], 0, 2));
+              mma<M>(o[2 * (c + h) + 1], pf[s16], widen<STORE, false>(vf[2 * h], 1, 3), widen<STORE, false>(vf[2 * h + 1], 1, 3));
             }
           }
+        } else {
+#pragma unroll
+          for (int c = 0; c < L::kChunks; c += 2) {
+            uint32_t vf[4];
+            ldm4t(vf, tc::smem_u32(vbase + swizzled<L::kRow, kKeys>(row0 + (lane & 15), c + (lane >> 4))));
+            mma<M>(o[c], pf[s16], vf[0], vf[1]);
+            mma<M>(o[c + 1], pf[s16], vf[2], vf[3]);
+          }
         }
       }
-      const bool whole = last && began >= 0;
-      if (wk == 0) {
+      // ---- the item's end, or the share's ----
+      const bool last = flags & kEnds;
+      if (last || u + 1 == count) {
+        const int4 b = say[1];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int in = wm * 16 + g + 8 * i, r = at.tile * ROWS + in;
-          if (r < at.r.rows) {
-            if (whole) {
-              const float inv = sum[i] > 0.f ? 1.f / sum[i] : (sum[i] == sum[i] ? 0.f : sum[i]);
-              const long long token = token_of(p, at.r.q0, r);
-              const int qh = head_of(p, at.h, r);
-              T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM;
-              if constexpr (k8) {
+          sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+          sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+        }
+        // warps that shared the keys: the upper half hands its rows to the lower one, until one has all; through the unit's own
+        // stage, which is not given back before
 #pragma unroll
-                for (int j = 0; j < DIM / 8; j += 2)
-                  *reinterpret_cast<uint2*>(out + j * 8 + 4 * tq) = make_uint2(pack2of<T>(o[j][2 * i] * inv, o[j + 1][2 * i] * inv),
-                                                                              pack2of<T>(o[j][2 * i + 1] * inv, o[j + 1][2 * i + 1] * inv));
-              } else {
+        for (int half = kWarpsK / 2; half > 0; half >>= 1) {
+          meet();
+          const int which = kWarpsK == 4 ? (wk & (half - 1)) : wm;
+          float* box = reinterpret_cast<float*>(smem + stage * L::kStage) + which * 16 * DIM;
+          if (wk >= half && wk < 2 * half) {
 #pragma unroll
-                for (int j = 0; j < DIM / 8; ++j)
-                  *reinterpret_cast<uint32_t*>(out + j * 8 + 2 * tq) = pack2of<T>(o[j][2 * i] * inv, o[j][2 * i + 1] * inv);
-              }
-              if (p.lse && tq == 0)
-                p.lse[token * p.q_heads + qh] = 0.69314718055994531f * ((top[i] == -INFINITY ? 0.f : top[i]) + log2f(sum[i]));
-            } else {
-              float* slot = p.part + (2 * share + (began >= 0)) * (long long)(ROWS * (DIM + 2));
-              float* x = slot + in * DIM;
-              if constexpr (k8) {
+            for (int i = 0; i < 2; ++i) {
+              float* x = box + (g + 8 * i) * DIM;
 #pragma unroll
-                for (int j = 0; j < DIM / 8; j += 2)
-                  *reinterpret_cast<float4*>(x + j * 8 + 4 * tq) = make_float4(o[j][2 * i], o[j + 1][2 * i], o[j][2 * i + 1], o[j + 1][2 * i + 1]);
-              } else {
+              for (int j = 0; j < DIM / 8; ++j) *reinterpret_cast<float2*>(x + ((j ^ g) * 8 + 2 * tq)) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
+              if (tq == 0) box_ts[which * 16 + g + 8 * i] = make_float2(top[i], sum[i]);
+            }
+          }
+          meet();
+          if (wk < half) {
 #pragma unroll
-                for (int j = 0; j < DIM / 8; ++j) *reinterpret_cast<float2*>(x + j * 8 + 2 * tq) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
-              }
-              if (tq == 0) {
-                slot[ROWS * DIM + in] = top[i];
-                slot[ROWS * (DIM + 1) + in] = sum[i];
+            for (int i = 0; i < 2; ++i) {
+              const float* x = box + (g + 8 * i) * DIM;
+              const float2 ts = box_ts[which * 16 + g + 8 * i];
+              const float both = fmaxf(top[i], ts.x), ref = both == -INFINITY ? 0.f : both;
+              const float a = ex2(top[i] - ref), c = ex2(ts.x - ref);
+              top[i] = both;
+              sum[i] = sum[i] * a + ts.y * c;
+#pragma unroll
+              for (int j = 0; j < DIM / 8; ++j) {
+                const float2 v = *reinterpret_cast<const float2*>(x + ((j ^ g) * 8 + 2 * tq));
+                o[j][2 * i] = o[j][2 * i] * a + v.x * c;
+                o[j][2 * i + 1] = o[j][2 * i + 1] * a + v.y * c;
               }
             }
           }
         }
+        if (kWarpsK > 1) fence_async_proxy();                  // before copies into the same place
+        const bool whole = last && (flags & kWholeStart);
+        if (wk == 0) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int in = wm * 16 + g + 8 * i, r = tile_row + in;
+            if (r < b.y) {
+              if (whole) {
+                const float inv = !ok ? __int_as_float(0x7fffffff) : sum[i] > 0.f ? 1.f / sum[i] : (sum[i] == sum[i] ? 0.f : sum[i]);
+                const long long token = token_of(p, q0, r);
+                const int qh = head_of(p, h, r);
+                T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM;
+                if constexpr (k8) {
+#pragma unroll
+                  for (int j = 0; j < DIM / 8; j += 2)
+                    *reinterpret_cast<uint2*>(out + j * 8 + 4 * tq) = make_uint2(pack2of<T>(o[j][2 * i] * inv, o[j + 1][2 * i] * inv),
+                                                                                pack2of<T>(o[j][2 * i + 1] * inv, o[j + 1][2 * i + 1] * inv));
+                } else {
+#pragma unroll
+                  for (int j = 0; j < DIM / 8; ++j)
+                    *reinterpret_cast<uint32_t*>(out + j * 8 + 2 * tq) = pack2of<T>(o[j][2 * i] * inv, o[j][2 * i + 1] * inv);
+                }
+                if (p.lse && tq == 0)
+                  p.lse[token * p.q_heads + qh] = ok ? 0.69314718055994531f * ((top[i] == -INFINITY ? 0.f : top[i]) + log2f(sum[i])) : inv;
+              } else {
+                float* slot = p.part + (2 * share + ((flags & kWholeStart) != 0)) * (long long)(ROWS * (DIM + 2));
+                float* x = slot + in * DIM;
+                if constexpr (k8) {
+#pragma unroll
+                  for (int j = 0; j < DIM / 8; j += 2)
+                    *reinterpret_cast<float4*>(x + j * 8 + 4 * tq) = make_float4(o[j][2 * i], o[j + 1][2 * i], o[j][2 * i + 1], o[j + 1][2 * i + 1]);
+                } else {
+#pragma unroll
+                  for (int j = 0; j < DIM / 8; ++j) *reinterpret_cast<float2*>(x + j * 8 + 2 * tq) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
+                }
+                if (tq == 0) {
+                  slot[ROWS * DIM + in] = top[i];
+                  slot[ROWS * (DIM + 1) + in] = ok ? sum[i] : __int_as_float(0x7fffffff);
+                }
+              }
+            }
+          }
+        }
+        if (u + 1 == count && tid == 0) {
+          const bool open = !last && (flags & kWholeStart);
+          p.open[2 * share] = make_int4(q0, h, tile_row, min(ROWS, b.y - tile_row));
+          p.open[2 * share + 1] = make_int4(open ? (int)((first + per + b.w - 1) / per) : -1, 0, 0, 0);
+        }
+        inside = false;
       }
-      if (u + 1 == count && tid == 0) {
-        const bool open = !last && began >= 0;
-        const long long end = first + began + at.units - 1;    // the item's last unit
-        p.open[2 * share] = make_int4(at.r.q0, at.h, at.tile * ROWS, min(ROWS, at.r.rows - at.tile * ROWS));
-        p.open[2 * share + 1] = make_int4(open ? (int)(end / per) : -1, 0, 0, 0);
-      }
-      fresh = true;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty + stage);
+      if (++stage == kS) { stage = 0; phase ^= 1u; }
     }
-    if (u + 1 < count) at.next(p);
-    stage = stage + 1 == kS ? 0 : stage + 1;
-    seen = seen == kS ? 0 : seen + 1;
+    if (!ok && inside && wk == 0) {                            // a wait gave up: the item at hand becomes NaN
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = tile_row + wm * 16 + g + 8 * i;
+        if (pos[i] < 0) continue;
+        T* out = static_cast<T*>(p.out) + token_of(p, q0, r) * p.out_ld + (long long)head_of(p, h, r) * DIM;
+        const uint32_t nan = pack2of<T>(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
+        for (int j = tq; j < DIM / 2; j += 4) reinterpret_cast<uint32_t*>(out)[j] = nan;
+      }
+    }
   }
   launch_dependents_now();
 }

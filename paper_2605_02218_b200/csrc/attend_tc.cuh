@@ -80,7 +80,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   f32x2 r;
@@ -127,22 +126,10 @@ __device__ __forceinline__ int tile_at(int rows, int row, int chunk) {
   return (chunk >> 3) * rows * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
 }
 
-__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-      ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-      : "memory");
-}
-
 template <typename T> __device__ __forceinline__ T pack_nan() {
   const uint32_t w = pack2of<T>(__int_as_float(0x7fffffff), 0.f);
   return *reinterpret_cast<const T*>(&w);
 }
-
-// What the producers tell the others of a unit: {first key, flags, first token of the request, head}, {first row of the item, rows of
-// the request, position of its first token, units of the item behind this one}.
-constexpr int kBegins = 1, kEnds = 2, kTwo = 4, kWholeStart = 8;   // first unit of its item in this share; last one of the item; rows
-                                                                   // in both tiles; the item's first unit is in this share
 
 template <typename T, int STORE, int DIM>
 __global__ void __launch_bounds__(kThreads, 1)

@@ -38,7 +38,7 @@ cudaError_t allow_shared(int bytes) {
 int check_cache(const covspec_cache* c) {
   if (!c || !c->k || !c->v) return COVSPEC_ERR_ARG;
   if (c->store < COVSPEC_F32 || c->store > COVSPEC_INT8) return COVSPEC_ERR_ARG;
-  if (c->store >= COVSPEC_E4M3 && (!c->k_scale || !c->v_scale)) return COVSPEC_ERR_ARG;
+  if (c->store >= COVSPEC_E4M3 && (!c->k_scale || !c->v_scale || !aligned16(c->k_scale) || !aligned16(c->v_scale))) return COVSPEC_ERR_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return COVSPEC_ERR_UNSUPPORTED;
   if (c->page_size < 8 || c->page_size > 4096 || (c->page_size & (c->page_size - 1))) return COVSPEC_ERR_UNSUPPORTED;
   if (c->pages < 1 || c->heads < 1 || (long long)c->heads * c->page_size * c->head_dim > INT_MAX) return COVSPEC_ERR_SHAPE;
@@ -103,33 +103,39 @@ int cache_grid(int rows, int lanes, int passes) {
 constexpr int kFewRows = 64, kRowsCtas = 2;
 long long part_bytes(int ctas, int rows, int dim) { return 2ll * ctas * rows * (dim + 2) * 4; }
 
-template <typename T, int STORE, int DIM, int ROWS>
-cudaError_t launch_rows(const attend::Params& prm, int ctas, cudaStream_t s) {
-  constexpr auto kernel = attend::attend_kernel<T, STORE, DIM, ROWS>;
-  constexpr int smem = attend::Layout<STORE, DIM, ROWS>::kSmem;
-  cudaError_t e = allow_shared<kernel>(smem);
-  if (e != cudaSuccess) return e;
-  e = launch_dependent(kernel, dim3((unsigned)ctas), attend::kThreads, smem, s, prm);
-  if (e != cudaSuccess) return e;
-  return launch_dependent(attend::attend_join_kernel<T, ROWS, DIM>, dim3((unsigned)ctas, ROWS / 4), 128, 0, s, prm);
-}
-
-// The keys or the values of a 16-bit cache as [pages, heads * page_size, dim]: boxes of 64 features of a page's rows of one head, in
-// tiles of 128-byte rows with the 128-byte swizzle.
-bool make_page_map(CUtensorMap* map, const covspec_cache* c, const void* base, long long page_stride) {
+// The keys or the values of a cache as [pages, heads * page_size, dim]: boxes of a page's rows of one head, at most `keys`, 128 bytes
+// wide (64 where a row has no more), in tiles with the swizzle of that width.
+bool make_page_map(CUtensorMap* map, const covspec_cache* c, const void* base, long long page_stride, int keys) {
   EncodeTiledFn encode = encode_tiled_fn();
   if (!encode) {
     g_cuda_error = "cuTensorMapEncodeTiled is not available";
     return false;
   }
+  const int e = bytes_of(c->store);
   const cuuint64_t dims[3] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->heads * c->page_size, (cuuint64_t)c->pages};
-  const cuuint64_t strides[2] = {(cuuint64_t)c->head_dim * 2, (cuuint64_t)page_stride * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)std::min(c->page_size, 128), 1}, step[3] = {1, 1, 1};
-  const CUresult r = encode(map, c->store == COVSPEC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
-                            const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  const cuuint64_t strides[2] = {(cuuint64_t)c->head_dim * e, (cuuint64_t)page_stride * e};
+  const cuuint32_t width = (cuuint32_t)std::min(c->head_dim * e, 128);
+  const cuuint32_t box[3] = {width / e, (cuuint32_t)std::min(c->page_size, keys), 1}, step[3] = {1, 1, 1};
+  const CUresult r = encode(map, e == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3,
+                            const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) g_cuda_error = "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r);
   return r == CUDA_SUCCESS;
+}
+
+template <typename T, int STORE, int DIM, int ROWS>
+cudaError_t launch_rows(const attend::Params& prm, const covspec_cache* cache, int ctas, cudaStream_t s) {
+  constexpr auto kernel = attend::attend_kernel<T, STORE, DIM, ROWS>;
+  using L = attend::Layout<STORE, DIM, ROWS>;
+  cudaError_t e = allow_shared<kernel>(L::kSmem);
+  if (e != cudaSuccess) return e;
+  CUtensorMap map_k, map_v;
+  if (!make_page_map(&map_k, cache, cache->k, cache->k_page_stride, L::kKeys) || !make_page_map(&map_v, cache, cache->v, cache->v_page_stride, L::kKeys))
+    return cudaErrorInvalidValue;
+  e = launch_dependent(kernel, dim3((unsigned)ctas), attend::kThreads, L::kSmem, s, map_k, map_v, prm);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(attend::attend_join_kernel<T, ROWS, DIM>, dim3((unsigned)ctas, ROWS / 4), 128, 0, s, prm);
 }
 
 template <typename T, int STORE, int DIM>
@@ -139,7 +145,7 @@ cudaError_t launch_wide(const attend::Params& prm, const covspec_cache* cache, i
   cudaError_t e = allow_shared<kernel>(smem);
   if (e != cudaSuccess) return e;
   CUtensorMap map_k{}, map_v{};
-  if (STORE < cache::kE4M3 && (!make_page_map(&map_k, cache, cache->k, cache->k_page_stride) || !make_page_map(&map_v, cache, cache->v, cache->v_page_stride)))
+  if (STORE < cache::kE4M3 && (!make_page_map(&map_k, cache, cache->k, cache->k_page_stride, attend::wide::kKeys) || !make_page_map(&map_v, cache, cache->v, cache->v_page_stride, attend::wide::kKeys)))
     return cudaErrorInvalidValue;
   e = launch_dependent(kernel, dim3((unsigned)ctas), attend::wide::kThreads, smem, s, map_k, map_v, prm);
   if (e != cudaSuccess) return e;
@@ -275,8 +281,8 @@ int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* token
         constexpr int kStore = decltype(store)::value;
         if (both)
           if (const cudaError_t e = launch_wide<T, kStore, kDim>(wide, cache, wide_ctas, s); e != cudaSuccess) return e;
-        return rows == 16 ? launch_rows<T, kStore, kDim, 16>(prm, ctas, s)
-               : rows == 32 ? launch_rows<T, kStore, kDim, 32>(prm, ctas, s) : launch_rows<T, kStore, kDim, 64>(prm, ctas, s);
+        return rows == 16 ? launch_rows<T, kStore, kDim, 16>(prm, cache, ctas, s)
+               : rows == 32 ? launch_rows<T, kStore, kDim, 32>(prm, cache, ctas, s) : launch_rows<T, kStore, kDim, 64>(prm, cache, ctas, s);
       };
       return cache->store == COVSPEC_E4M3 ? of_store(Const<cache::kE4M3>())
              : cache->store == COVSPEC_INT8 ? of_store(Const<cache::kInt8>()) : of_store(Const<kOwn>());
