@@ -132,6 +132,11 @@ __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, ui
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(tc::smem_u32(bar)) : "memory");
 }
+// A wait of the whole warp: its lanes leave the polls one by one, and the instructions that follow want them together.  Nothing here
+// waits for more than what its own CTA has under way, so it gives up early.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, tc::mbar_wait_limited(bar, parity, abort_flag, 1u << 18));
+}
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <typename T, int STORE, int DIM, int ROWS>
@@ -209,7 +214,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         at.next(p);
         look_up();
       }
-      if (!(ok = mbar_wait(empty + stage, phase, abort_flag))) break;
+      if (!(ok = warp_wait(empty + stage, phase, abort_flag))) break;
       char* base = smem + stage * L::kStage;
       float* sc = reinterpret_cast<float*>(smem + kS * L::kStage) + stage * 2 * kKeys;
       uint64_t* bar = all == 0xffffffffu ? full + stage : partly;
@@ -231,7 +236,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                     rows * 4, bar);
       }
       if (all != 0xffffffffu) {                                // values of keys that are not there: zeros, whatever memory holds
-        if (!(ok = mbar_wait(partly, part_phase, abort_flag))) break;
+        if (!(ok = warp_wait(partly, part_phase, abort_flag))) break;
         part_phase ^= 1u;
 #pragma unroll
         for (int i = 0; i < kKeys / 32; ++i)
@@ -268,11 +273,11 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     auto meet = [&] {
       __syncwarp();
       if (lane == 0) mbar_arrive(met);
-      ok = mbar_wait(met, met_phase, abort_flag) && ok;
+      ok = warp_wait(met, met_phase, abort_flag) && ok;
       met_phase ^= 1u;
     };
     for (int u = 0; u < count; ++u) {
-      if (!(ok = mbar_wait(full + stage, phase, abort_flag) && ok)) break;
+      if (!(ok = warp_wait(full + stage, phase, abort_flag) && ok)) break;
       const int4* say = reinterpret_cast<const int4*>(says + stage * L::kSay);
       const uint32_t* there = reinterpret_cast<const uint32_t*>(say + 2);
       const int flags = say[0].y;

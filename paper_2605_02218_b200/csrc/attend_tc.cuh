@@ -6,16 +6,13 @@
 // MN-major (keys are the inner dimension of the second product), both as rows of 64 features in 128-byte swizzled tiles.
 //
 // Warps: 0-7 and 8-15 softmax of tile 0 and 1, a row of it two threads in two warps, each half of a unit's keys; 16 issues the
-// products; 17-19 bring queries, keys and values into shared memory.  16-bit keys and values come by tiled copies, a box as many rows
-// as a page has (at most 128), issued by one warp, a box a lane; where not every key of a unit is there, the values' other rows
-// are cleared before the products may see them.  8-bit ones come through registers, where they are widened (attend_kernels.cuh).
+// products; 17-19 bring queries, and 17 keys and values, into shared memory: tiled copies, a box as many rows as a page has (at most
+// 128), a box a lane.  Where not every key of a unit is there, the values' other rows are cleared before the products may see them.
 //
 // The running maximum is only a reference that keeps the exponentials in range: a row keeps it
 // while a unit's probabilities add up to at most 2^14, so that O is rescaled seldom and one pass over S makes the probabilities.  A
 // warp with a row beyond that goes over S again with new references.
 #pragma once
-#include <type_traits>
-
 #include "attend_kernels.cuh"
 
 namespace covspec {
@@ -31,15 +28,12 @@ constexpr int kOpen = 4;                    // units that beginning and ending a
 constexpr float kMost = 16384.f;            // a unit's probabilities add up to no more over their reference
 
 template <int STORE, int DIM> struct Layout {
-  static constexpr bool k8 = STORE >= cache::kE4M3;
+  static_assert(STORE < cache::kE4M3);
   static constexpr int kSlot = kKeys * DIM * 2;                // keys or values of a unit, 16-bit
-  static constexpr int kRow = DIM * (k8 ? 1 : 2);              // bytes of a row in the cache
   static constexpr int kQ = kRows * DIM * 2;
-  static constexpr int kSlots = k8 ? 4 : 5;
+  static constexpr int kSlots = 5;
   static constexpr int kTail = 4 * 16 + 4 * 32                 // which keys of a unit are there, its item; 4 units
-                               + (k8 ? 4 * 2 * kKeys * 4 + 2 * kRows * 4 : 0)   // scales of 4 units; of the query rows of 2 items
-                               + 2 * kKeys * 4                 // pages of a unit's keys, 2 units
-                               + 256 + 2 * 128 * 4;            // barriers, TMEM base; exchange
+                               + 256 + 2 * 128 * 4;            // barriers, TMEM base; exchange, first the scratch of find_share
   static constexpr int kUsed = kQ + kSlots * kSlot + kTail;
   static constexpr int kSmem = kUsed > 120 * 1024 ? kUsed : 120 * 1024;      // one CTA an SM: each takes all of TMEM
   static_assert(kSmem <= 232448);
@@ -94,27 +88,36 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 
-// Barrier among `n` threads that tells each whether all came with `v`.
+// Barriers among `n` threads.  Not the aligned forms: those want the warp's lanes together, which nothing after a branch on the lane
+// promises; with them a large call of one build stood still.
+__device__ __forceinline__ void meet_at(int id, int n) {
+  __syncwarp();
+  asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(n) : "memory");
+}
+// It tells each whether all came with `v`, ...
 __device__ __forceinline__ bool barrier_and(int id, int n, bool v) {
   uint32_t r;
+  __syncwarp();
   asm volatile(
       "{\n"
       ".reg .pred p, q;\n"
       "setp.ne.u32 p, %3, 0;\n"
-      "barrier.cta.red.and.aligned.pred q, %1, %2, p;\n"
+      "barrier.cta.red.and.pred q, %1, %2, p;\n"
       "selp.u32 %0, 1, 0, q;\n"
       "}\n"
       : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)v) : "memory");
   return r != 0;
 }
 
+// ... whether one did.
 __device__ __forceinline__ bool barrier_or(int id, int n, bool v) {
   uint32_t r;
+  __syncwarp();
   asm volatile(
       "{\n"
       ".reg .pred p, q;\n"
       "setp.ne.u32 p, %3, 0;\n"
-      "barrier.cta.red.or.aligned.pred q, %1, %2, p;\n"
+      "barrier.cta.red.or.pred q, %1, %2, p;\n"
       "selp.u32 %0, 1, 0, q;\n"
       "}\n"
       : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)v) : "memory");
@@ -135,9 +138,6 @@ template <typename T, int STORE, int DIM>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p) {
   using L = Layout<STORE, DIM>;
-  constexpr bool k8 = L::k8;
-  using M = std::conditional_t<k8, __half, T>;                 // type of the products
-  constexpr bool kConvert = !__is_same(M, T);                  // queries to float16
   constexpr int kSlots = L::kSlots;
   extern __shared__ __align__(1024) uint8_t wide_smem[];
   uint8_t* smem = wide_smem;
@@ -145,10 +145,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   uint8_t* tail = ring + kSlots * L::kSlot;
   uint32_t* there = reinterpret_cast<uint32_t*>(tail);                       // [4][4]
   int4* units = reinterpret_cast<int4*>(tail + 64);                          // [4][2], see below
-  float* scales = reinterpret_cast<float*>(tail + 192);                       // [4][2][kKeys]: key scale, value scale
-  float* row_scales = scales + 4 * 2 * kKeys;                                // [2][kRows]
-  int* pages = reinterpret_cast<int*>(tail + 192 + (k8 ? 4 * 2 * kKeys * 4 + 2 * kRows * 4 : 0));   // [2][kKeys]: of a unit's keys, -1: none
-  uint64_t* bars = reinterpret_cast<uint64_t*>(pages + 2 * kKeys);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(tail + 192);
   float* exchange = reinterpret_cast<float*>(bars + 32);                     // [2][128]: between the two threads of a row
   uint64_t *full = bars, *empty = bars + 5, *q_full = bars + 10, *q_empty = bars + 11, *s_full = bars + 12, *p_ready = bars + 14,
            *o_full = bars + 16, *drained = bars + 18, *partly = bars + 19;   // 20 barriers
@@ -156,7 +153,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, k8 ? kProducers : 1); mbar_init(empty + i, 1); }
+    for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
     mbar_init(q_full, kProducers);
     mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) { mbar_init(s_full + i, 1); mbar_init(p_ready + i, 8); mbar_init(o_full + i, 1); }
@@ -168,7 +165,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   wait_for_previous_kernel();
   Cursor<kRows, kKeys> at;
   long long first, per;
-  const int count = find_share<kRows, kKeys, kThreads, kOpen>(p, at, first, per, reinterpret_cast<long long*>(pages));
+  const int count = find_share<kRows, kKeys, kThreads, kOpen>(p, at, first, per, reinterpret_cast<long long*>(exchange));
   const int share = blockIdx.x;
   if (count <= 0) {
     if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
@@ -184,7 +181,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
   if (warp > kSoftmaxWarps) {
     // ---------------- producers ----------------
-    const int t = tid - (kSoftmaxWarps + 1) * 32, wp = warp - kSoftmaxWarps - 1;
+    const int wp = warp - kSoftmaxWarps - 1;
     uint64_t* waiting[3] = {nullptr, nullptr, nullptr};        // barriers of copies that are under way, the oldest last
     auto close = [&](uint64_t* bar) {                          // the copies so far belong to `bar`
       copies_close();
@@ -204,25 +201,14 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     };
     // nothing is waited for while copies that the others may need to get on have not been handed over
     auto acquire = [&](uint64_t* bar, uint32_t parity) {
-      if (mbar_peek(bar, parity)) return true;
+      if (__all_sync(0xffffffffu, mbar_peek(bar, parity))) return true;
       flush();
-      return mbar_wait(bar, parity, abort_flag);
+      return warp_wait(bar, parity, abort_flag);
     };
     int slot = 0;
     uint32_t phase = 1, q_phase = 1;
     bool ok = true, fresh = true;
-    [[maybe_unused]] int items = 0;
     auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
-    int page[2] = {-1, -1};                                    // of keys t and, in the first warp, t + 96
-    bool whole_start = false;
-    auto look_up = [&] {                                       // of the unit at `at`
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int key = at.key + t + i * kProducers;
-        const bool mine = (i == 0 || wp == 0) && key >= at.k.lo && key < at.k.hi;
-        page[i] = mine ? p.t.table[at.b * p.t.table_ld + (key >> p.c.page_shift)] : -1;
-      }
-    };
     auto queries = [&] {                                       // of the item at `at`
       ok = ok && acquire(q_empty, q_phase);
       q_phase ^= 1u;
@@ -241,24 +227,11 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         head += step_head;
         if (head >= p.group) { head -= p.group; ++token; }
         uint8_t* to = smem + (row >> 7) * (128 * DIM * 2) + tile_at(128, row & 127, chunk);
-        if constexpr (!kConvert) {
-          if (in) copy16(smem_u32(to), q, is);
-        } else {
-          const uint4 w = is ? *reinterpret_cast<const uint4*>(q) : make_uint4(0u, 0u, 0u, 0u);
-          float most = largest_of(w.x, largest_of(w.y, largest_of(w.z, largest_of(w.w, 0.f))));
-#pragma unroll
-          for (int o = kChunks / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-          const float f = power_for(most);
-          if (in) {
-            *reinterpret_cast<uint4*>(to) = make_uint4(to_half(w.x, f), to_half(w.y, f), to_half(w.z, f), to_half(w.w, f));
-            if (chunk == 0) row_scales[items * kRows + row] = inverse_power(f);
-          }
-        }
+        if (in) copy16(smem_u32(to), q, is);
       }
-      items ^= 1;
       close(q_full);
     };
-    if constexpr (!k8) {
+    {
       if (wp > 0) {                                            // these two only help with the queries
         for (int u = 0; u < count && ok; ++u) {
           if (fresh) {
@@ -306,7 +279,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             look_up_box();
           }
           // the words of unit u - 4 have been read: its products are done (the slot that this unit's keys take says so)
-          if (!(ok = mbar_wait(empty + slot, phase, abort_flag))) break;
+          if (!(ok = warp_wait(empty + slot, phase, abort_flag))) break;
           if (lane == 0) {
             *reinterpret_cast<uint4*>(there + (u & 3) * 4) = make_uint4(word[0], word[1], word[2], word[3]);
             units[(u & 3) * 2] = item[0];
@@ -316,14 +289,14 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           __syncwarp();
           if (mine) tma_load_3d(smem_u32(ring + slot * L::kSlot) + part * (kKeys * 128) + (box << shift) * 128, &map_k, part * 64, page_row, box_page, full + slot);
           next_slot();
-          if (!(ok = mbar_wait(empty + slot, phase, abort_flag))) break;
+          if (!(ok = warp_wait(empty + slot, phase, abort_flag))) break;
           const bool all = (word[0] & word[1] & word[2] & word[3]) == 0xffffffffu;
           uint64_t* bar = all ? full + slot : partly;
           if (lane == 0) mbar_expect_tx(bar, bytes);
           __syncwarp();
           if (mine) tma_load_3d(smem_u32(ring + slot * L::kSlot) + part * (kKeys * 128) + (box << shift) * 128, &map_v, part * 64, page_row, box_page, bar);
           if (!all) {                                          // values of keys that are not there: zeros, whatever memory holds
-            ok = mbar_wait(partly, part_phase, abort_flag);
+            ok = warp_wait(partly, part_phase, abort_flag);
             part_phase ^= 1u;
             if (!ok) break;
 #pragma unroll
@@ -344,102 +317,10 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           mbar_wait_limited(full + i, 1, &gave_up, 1u << 16);
         }
       }
-    } else {
-    look_up();
-    for (int u = 0; u < count; ++u) {
-      if (fresh) queries();
-      // pages of the unit's keys; those of the next unit's are under way meanwhile
-      int* unit_pages = pages + (u & 1) * kKeys;
-      const int mask = (1 << p.c.page_shift) - 1, key0 = at.key, first_row = at.h << p.c.page_shift;
-      {
-        int has[2];
-        [[maybe_unused]] float ks[2] = {0.f, 0.f}, vs[2] = {1.f, 1.f};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          has[i] = (unsigned)page[i] < (unsigned)p.c.pages ? page[i] : -1;
-          if constexpr (k8) {
-            const long long w = (((long long)has[i] * p.c.heads) << p.c.page_shift) + first_row + ((key0 + t + i * kProducers) & mask);
-            if (has[i] >= 0) {
-              ks[i] = p.c.k_scale[w];
-              vs[i] = p.c.v_scale[w];
-            }
-          }
-        }
-        const int row0 = at.tile * kRows;
-        const bool begins = fresh;
-        if (begins) whole_start = at.unit == 0;
-        fresh = at.unit + 1 == at.units;
-        const int4 item[2] = {make_int4(at.key, (begins ? kBegins : 0) | (fresh ? kEnds : 0) | (at.r.rows - row0 > 128 ? kTwo : 0) | (whole_start ? kWholeStart : 0), at.r.q0, at.h),
-                              make_int4(row0, at.r.rows, at.r.length - at.r.n, at.units - 1 - at.unit)};
-        if (u + 1 < count) {
-          at.next(p);
-          look_up();
-        }
-        // the words of unit u - 4 have been read: its products are done (the slot that this unit's keys take says so)
-        ok = ok && acquire(empty + slot, phase);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int key = t + i * kProducers;
-          if (i == 1 && wp != 0) break;
-          unit_pages[key] = has[i];
-          const uint32_t word = __ballot_sync(0xffffffffu, has[i] >= 0);
-          if (lane == 0) there[(u & 3) * 4 + (key >> 5)] = word;
-          if constexpr (k8) {
-            float* sc = scales + (u & 3) * 2 * kKeys;
-            sc[key] = ks[i];
-            sc[kKeys + key] = vs[i] < cache::kLeastScale ? cache::kLeastScale : vs[i];
-          }
-        }
-        if (t == 0) {
-          units[(u & 3) * 2] = item[0];
-          units[(u & 3) * 2 + 1] = item[1];
-        }
-      }
-      // all of them go on or none: a thread that has left would be waited for at the next barrier
-      if (!(ok = barrier_and(1, kProducers, ok))) break;
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        if (kv && !(ok = acquire(empty + slot, phase))) break;
-        uint8_t* dst = ring + slot * L::kSlot;
-        constexpr int kChunks = L::kRow / 16, kAtOnce = 32 / kChunks, kPer = (kKeys / kAtOnce + kCopyWarps - 1) / kCopyWarps;
-        const int chunk = lane % kChunks;
-        const char* base = static_cast<const char*>(kv ? p.c.v : p.c.k) + chunk * 16;
-        auto row_of = [&](int i) { return (wp + kCopyWarps * i) * kAtOnce + lane / kChunks; };
-        int has[kPer];                                         // read ahead: no load passes a copy
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) has[i] = row_of(i) < kKeys ? unit_pages[row_of(i)] : -1;
-        const long long page_bytes = (kv ? p.c.v_page : p.c.k_page) * (L::kRow / DIM);
-        auto source = [&](int i) { return base + has[i] * page_bytes + (long long)(first_row + ((key0 + row_of(i)) & mask)) * L::kRow; };
-        {
-          uint4 raw[kPer];
-#pragma unroll
-          for (int i = 0; i < kPer; ++i)
-            raw[i] = has[i] >= 0 ? *reinterpret_cast<const uint4*>(source(i)) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-          for (int i = 0; i < kPer; ++i) {
-            const int row = row_of(i);
-            if (i == kPer - 1 && row >= kKeys) break;
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-            uint32_t v[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              v[2 * e] = widen<STORE, true>(w[e], 0, 1);
-              v[2 * e + 1] = widen<STORE, false>(w[e], 2, 3);
-            }
-            *reinterpret_cast<uint4*>(dst + tile_at(kKeys, row, 2 * chunk)) = make_uint4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<uint4*>(dst + tile_at(kKeys, row, 2 * chunk + 1)) = make_uint4(v[4], v[5], v[6], v[7]);
-          }
-          flush();                                             // the queries' copies, if they are still under way
-          mbar_arrive(full + slot);
-        }
-        next_slot();
-      }
-    }
-    flush();
     }
   } else if (warp == kSoftmaxWarps) {
     // ---------------- products ----------------
-    const uint32_t qk = idesc<M>(kKeys, false), pv = idesc<M>(DIM, true);
+    const uint32_t qk = idesc<T>(kKeys, false), pv = idesc<T>(DIM, true);
     int slot = 0;
     uint32_t phase = 0, q_phase = 0, p_phase = 0;
     bool ok = true;
@@ -462,9 +343,9 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     bool opened = false;                                       // the unit's scores are issued
     for (int u = 0; u < count && ok; ++u) {
       if (!opened) {                                           // it begins an item here
-        ok = mbar_wait(q_full, q_phase, abort_flag);
+        ok = warp_wait(q_full, q_phase, abort_flag);
         q_phase ^= 1u;
-        ok = ok && mbar_wait(full + slot, phase, abort_flag);
+        ok = ok && warp_wait(full + slot, phase, abort_flag);
         if (!ok) break;
         tc_fence_after();
         if (lane == 0) {
@@ -480,13 +361,13 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const bool two = flags & kTwo, more = u + 1 < count && !(flags & kEnds);
       if (!more && lane == 0) umma_commit(q_empty);
       const int v_slot = slot;
-      ok = mbar_wait(full + v_slot, phase, abort_flag);
+      ok = warp_wait(full + v_slot, phase, abort_flag);
       if (!ok) break;
       next_slot();
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        ok = ok && mbar_wait(p_ready + x, p_phase, abort_flag);
-        if (x == 0 && more) ok = ok && mbar_wait(full + slot, phase, abort_flag);
+        ok = ok && warp_wait(p_ready + x, p_phase, abort_flag);
+        if (x == 0 && more) ok = ok && warp_wait(full + slot, phase, abort_flag);
         if (!ok) break;
         tc_fence_after();
         if (lane == 0) {
@@ -513,7 +394,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     // TMEM and the ring are free when every product has ended, also after a wait that gave up
     if (lane == 0) umma_commit(drained);
     volatile int gave_up = 0;
-    mbar_wait(drained, 0, &gave_up);
+    warp_wait(drained, 0, &gave_up);
     __syncwarp();
   } else {
     // ---------------- softmax ----------------
@@ -522,14 +403,14 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;
     const uint32_t s_at = tmem + lanes + x * 128, o_at = tmem + lanes + kO + x * 128 + half * (DIM / 2);
     float* shared = exchange + x * 128 + row;
-    float ref = 0.f, sum = 0.f, row_scale = 0.f;
-    int pos = -1, items = 0;                                   // position of the row's token; items so far, the parity
+    float ref = 0.f, sum = 0.f;
+    int pos = -1;                                              // position of the row's token
     bool ok = true, active = false;
     uint32_t s_phase = 0, o_phase = 0;
     if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
     for (int u = 0; u < count; ++u) {
       // the two warps of a row go on or give up together: they meet at barriers further down
-      ok = barrier_and(pair, 64, mbar_wait(s_full + x, s_phase, abort_flag));
+      ok = barrier_and(pair, 64, warp_wait(s_full + x, s_phase, abort_flag));
       if (!ok) {                                               // it gave up: the item at hand becomes NaN
         const int4 first_half = units[((u - 1) & 3) * 2], item = units[((u - 1) & 3) * 2 + 1];
         const int r = item.x + x * 128 + row;
@@ -540,6 +421,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
       s_phase ^= 1u;
       tc_fence_after();
+      __syncwarp();
       const int key = units[(u & 3) * 2].x, flags = units[(u & 3) * 2].y;
       if (flags & kBegins) {
         const int4 item = units[(u & 3) * 2 + 1];
@@ -549,15 +431,12 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         pos = is ? item.z + r / p.group : 0x7fffffff;          // no row: nothing to mask, no reference to look for
         ref = is ? -INFINITY : 0.f;
         sum = 0.f;
-        row_scale = kConvert ? row_scales[items * kRows + x * 128 + row] * p.scale_log2 : p.scale_log2;
-        items ^= 1;
       }
       if (!active) {
         __syncwarp();
         if (lane == 0) mbar_arrive(p_ready + x);
       } else {
         const uint4 bits = *reinterpret_cast<const uint4*>(there + (u & 3) * 4);
-        const float* sc = scales + (u & 3) * 2 * kKeys + half * 64;
         // every row of the warp sees all keys of the unit
         const bool clear = (bits.x & bits.y & bits.z & bits.w) == 0xffffffffu &&
                            __all_sync(0xffffffffu, key + kKeys - 1 <= pos && (p.window == 0 || pos == 0x7fffffff || key > pos - p.window));
@@ -571,7 +450,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           return see;
         };
         uint32_t packed[32];
-        float more, most;                                      // sums of the probabilities, without and with the values' scales
+        float more;                                            // sum of the probabilities
         bool renew = __any_sync(0xffffffffu, ref == -INFINITY);  // the same in both halves
         for (;;) {
           if (renew) {                                         // new references, from the scores themselves
@@ -583,15 +462,13 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
               const uint32_t see = seen(c / 2) >> (16 * (c & 1));
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
-                const int at = 16 * c + e;
-                const float t = k8 ? v[e] * (sc[at] * row_scale) + log2f(sc[kKeys + at]) : v[e] * row_scale;
-                best = (see >> e) & 1u ? fmaxf(best, t) : best;
+                best = (see >> e) & 1u ? fmaxf(best, v[e] * p.scale_log2) : best;
               }
             }
             if (half) *shared = best;
-            named_barrier(pair, 64);
+            meet_at(pair, 64);
             if (!half) *shared = best = fmaxf(best, *shared);
-            named_barrier(pair, 64);
+            meet_at(pair, 64);
             if (half) best = *shared;
             const float shrink = ref == -INFINITY ? 0.f : ex2(ref - best);
             ref = best;
@@ -610,26 +487,18 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
           }
           const float safe = ref == -INFINITY ? 0.f : ref;
-          const f32x2 low = pack2(-safe, -safe), by = pack2(row_scale, row_scale);
+          __syncwarp();
+          const f32x2 low = pack2(-safe, -safe), by = pack2(p.scale_log2, p.scale_log2);
           f32x2 sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-          [[maybe_unused]] f32x2 most2 = pack2(0.f, 0.f);
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             float v[32];
             tmem_ld32(s_at + 64 * half + 32 * c, v);
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              f32x2 f[2] = {by, by};
-              if constexpr (k8) {
-                const float4 a = *reinterpret_cast<const float4*>(sc + 32 * c + e);
-                f[0] = mul2(pack2(a.x, a.y), by); f[1] = mul2(pack2(a.z, a.w), by);
-              }
-#pragma unroll
-              for (int i = 0; i < 4; i += 2) {
-                const float2 t = unpack2(fma2(pack2(v[e + i], v[e + i + 1]), f[i / 2], low));
-                v[e + i] = t.x;
-                v[e + i + 1] = t.y;
-              }
+            for (int e = 0; e < 32; e += 2) {
+              const float2 t = unpack2(fma2(pack2(v[e], v[e + 1]), by, low));
+              v[e] = t.x;
+              v[e + 1] = t.y;
             }
             if (!clear) {
               const uint32_t see = seen(c);
@@ -637,34 +506,21 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
               for (int e = 0; e < 32; ++e) v[e] = (see >> e) & 1u ? v[e] : -INFINITY;
             }
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              [[maybe_unused]] f32x2 g[2];
-              if constexpr (k8) {
-                const float4 b = *reinterpret_cast<const float4*>(sc + kKeys + 32 * c + e);
-                g[0] = pack2(b.x, b.y); g[1] = pack2(b.z, b.w);
-              }
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                f32x2 t2 = pack2(ex2(v[e + 2 * i]), ex2(v[e + 2 * i + 1]));
-                sum2[i] = add2(sum2[i], t2);
-                if constexpr (k8) {
-                  t2 = mul2(t2, g[i]);
-                  most2 = add2(most2, t2);
-                }
-                const float2 t = unpack2(t2);
-                packed[16 * c + e / 2 + i] = pack2of<M>(t.x, t.y);
-              }
+            for (int e = 0; e < 32; e += 2) {
+              const float x = ex2(v[e]), y = ex2(v[e + 1]);
+              sum2[e / 2 & 1] = add2(sum2[e / 2 & 1], pack2(x, y));
+              packed[16 * c + e / 2] = pack2of<T>(x, y);
             }
           }
-          const float2 a = unpack2(add2(sum2[0], sum2[1])), b = unpack2(most2);
+          const float2 a = unpack2(add2(sum2[0], sum2[1]));
           more = a.x + a.y;
-          most = k8 ? b.x + b.y : more;
           // both halves of the rows alike; and both have read their scores, over which the probabilities are written
-          const bool over = barrier_or(pair, 64, most > kMost);
+          const bool over = barrier_or(pair, 64, more > kMost);
           if (renew || !over) break;
           renew = true;
         }
         sum += more;
+        __syncwarp();
         tmem_st32(s_at + 32 * half, packed);
         tmem_st_wait();
         tc_fence_before();
@@ -676,16 +532,16 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const bool whole = (flags & kEnds) && (flags & kWholeStart);
         const int q0 = units[(u & 3) * 2].z, h = units[(u & 3) * 2].w;
         if (active) {
-          ok = mbar_wait(o_full + x, o_phase, abort_flag);
+          ok = warp_wait(o_full + x, o_phase, abort_flag);
           o_phase ^= 1u;
           tc_fence_after();
           const int r = item.x + x * 128 + row;
           const bool is = r < item.y;
           float total = sum;
           if (half) *shared = sum;
-          named_barrier(pair, 64);
+          meet_at(pair, 64);
           if (!half) *shared = total = sum + *shared;
-          named_barrier(pair, 64);
+          meet_at(pair, 64);
           if (half) total = *shared;
           // a wait that gave up leaves NaN
           const float inv = !ok ? __int_as_float(0x7fffffff) : total > 0.f ? 1.f / total : (total == total ? 0.f : total);

@@ -145,7 +145,7 @@ cudaError_t launch_wide(const attend::Params& prm, const covspec_cache* cache, i
   cudaError_t e = allow_shared<kernel>(smem);
   if (e != cudaSuccess) return e;
   CUtensorMap map_k{}, map_v{};
-  if (STORE < cache::kE4M3 && (!make_page_map(&map_k, cache, cache->k, cache->k_page_stride, attend::wide::kKeys) || !make_page_map(&map_v, cache, cache->v, cache->v_page_stride, attend::wide::kKeys)))
+  if (!make_page_map(&map_k, cache, cache->k, cache->k_page_stride, attend::wide::kKeys) || !make_page_map(&map_v, cache, cache->v, cache->v_page_stride, attend::wide::kKeys))
     return cudaErrorInvalidValue;
   e = launch_dependent(kernel, dim3((unsigned)ctas), attend::wide::kThreads, smem, s, map_k, map_v, prm);
   if (e != cudaSuccess) return e;
@@ -258,7 +258,7 @@ int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* token
   // rows of a key head in the largest request.  Where some may have many, each of the two kernels takes its requests
   const long long most = (long long)(max_new > 0 ? std::min(max_new, n) : n) * prm.group;
   const int rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
-  const bool both = most > kFewRows;
+  const bool both = most > kFewRows && cache->store < COVSPEC_E4M3;
   // no more CTAs than there can be units
   auto ctas_of = [&](int rows, int keys, int ctas) {
     const long long items = ((long long)n * prm.group / rows + prm.t.batch) * cache->heads;
@@ -279,8 +279,10 @@ int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* token
       constexpr int kDim = decltype(dim)::value;
       auto of_store = [&](auto store) {
         constexpr int kStore = decltype(store)::value;
-        if (both)
-          if (const cudaError_t e = launch_wide<T, kStore, kDim>(wide, cache, wide_ctas, s); e != cudaSuccess) return e;
+        if constexpr (kStore < cache::kE4M3) {
+          if (both)
+            if (const cudaError_t e = launch_wide<T, kStore, kDim>(wide, cache, wide_ctas, s); e != cudaSuccess) return e;
+        }
         return rows == 16 ? launch_rows<T, kStore, kDim, 16>(prm, cache, ctas, s)
                : rows == 32 ? launch_rows<T, kStore, kDim, 32>(prm, cache, ctas, s) : launch_rows<T, kStore, kDim, 64>(prm, cache, ctas, s);
       };
