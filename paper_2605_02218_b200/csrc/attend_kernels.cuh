@@ -19,6 +19,7 @@ namespace covspec {
 namespace attend {
 
 constexpr int kThreads = 160, kWarps = 4;        // threads of a CTA; its warps that compute
+constexpr int kOpen = 2;                         // units that beginning and ending an item costs (none: shares end up to 15 % apart)
 
 template <int STORE, int DIM, int ROWS> struct Layout {
   static constexpr bool k8 = STORE >= cache::kE4M3;
@@ -79,22 +80,17 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
 }
 
 // Two 8-bit values (bytes `lo` and `hi` of a word) as two float16, exactly.  8-bit keys and values are multiplied in float16
-// whatever the type of the queries: both widen to it in fewer instructions than to bfloat16 (four a pair), and probabilities
-// keep three more bits.  Queries in bfloat16 are brought to float16 by a power of two for each row (to_half).
-//  e4m3: the conversion instruction runs at about 8 values a cycle on an SM, so most pairs (!CVT) move their seven lower bits to
-//        where float16 has them, which is the value over 2^8, and multiply by that power, which is exact, subnormal codes
-//        included.  The code of NaN does not occur in a cache.
+// whatever the type of the queries: both widen to it in fewer instructions than to bfloat16, and probabilities keep three more
+// bits.  Queries in bfloat16 are brought to float16 by a power of two for each row (to_half).
+//  e4m3: the conversion instruction (half of the pairs by shifts and a product with 2^8 instead, exact too: 64 caches of 500-16384
+//        positions, 8 heads of 128, 138 -> 160 us; all of them 189).
 //  int8: the byte becomes the lower bits of 1024 + (v + 128), and 1152 is taken off.
-template <int STORE, bool CVT>
+template <int STORE>
 __device__ __forceinline__ uint32_t widen(uint32_t bytes, int lo, int hi) {
   uint32_t r;
-  if constexpr (STORE == cache::kE4M3 && CVT) {
-    const uint32_t two = lo + 1 == hi && lo == 0 ? bytes : __byte_perm(bytes, 0u, (uint32_t)(lo | hi << 4));
+  if constexpr (STORE == cache::kE4M3) {
+    const uint32_t two = lo == 0 && hi == 1 ? bytes : __byte_perm(bytes, 0u, (uint32_t)(lo | hi << 4));
     asm("{\n.reg .b16 h;\ncvt.u16.u32 h, %1;\ncvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(r) : "r"(two));
-  } else if constexpr (STORE == cache::kE4M3) {
-    const uint32_t w = __byte_perm(bytes, 0u, (uint32_t)(4 | lo << 4 | 4 << 8 | hi << 12));   // in the halves' upper bytes
-    const uint32_t m = (w & 0x80008000u) | ((w >> 1) & 0x3f803f80u);
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(0x5c005c00u));
   } else {
     const uint32_t w = __byte_perm(bytes ^ 0x80808080u, 0x64646464u, (uint32_t)(lo | 4 << 4 | hi << 8 | 4 << 12));
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x64806480u));
@@ -170,7 +166,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
   const int share = blockIdx.x;
   Cursor<ROWS, kKeys> at;
   long long first, per;
-  const int count = find_share<ROWS, kKeys, kThreads, 0>(p, at, first, per, scratch);
+  const int count = find_share<ROWS, kKeys, kThreads, kOpen>(p, at, first, per, scratch);
   if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
   if (count <= 0) {
     launch_dependents_now();
@@ -338,10 +334,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
           ldm4(kf, smem_u32(kbase + swizzled<L::kRow, kKeys>(row, c + (lane >> 3))));
           if constexpr (k8) {
 #pragma unroll
-            for (int i = 0; i < 4; i += 2) {                    // every other chunk by conversions: both units are kept busy
-              mma<M>(s[j], qf[c + i], widen<STORE, true>(kf[i], 0, 1), widen<STORE, true>(kf[i], 2, 3));
-              mma<M>(s[j], qf[c + i + 1], widen<STORE, false>(kf[i + 1], 0, 1), widen<STORE, false>(kf[i + 1], 2, 3));
-            }
+            for (int i = 0; i < 4; ++i) mma<M>(s[j], qf[c + i], widen<STORE>(kf[i], 0, 1), widen<STORE>(kf[i], 2, 3));
           } else {
             mma<M>(s[j], qf[c / 2], kf[0], kf[1]);
             mma<M>(s[j], qf[c / 2 + 1], kf[2], kf[3]);
@@ -419,8 +412,8 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               // a register holds features 2n, 2n + 1 of two keys: the even ones make one tile of eight columns, the odd ones another
-              mma<M>(o[2 * (c + h)], pf[s16], widen<STORE, false>(vf[2 * h], 0, 2), widen<STORE, false>(vf[2 * h + 1], 0, 2));
-              mma<M>(o[2 * (c + h) + 1], pf[s16], widen<STORE, false>(vf[2 * h], 1, 3), widen<STORE, false>(vf[2 * h + 1], 1, 3));
+              mma<M>(o[2 * (c + h)], pf[s16], widen<STORE>(vf[2 * h], 0, 2), widen<STORE>(vf[2 * h + 1], 0, 2));
+              mma<M>(o[2 * (c + h) + 1], pf[s16], widen<STORE>(vf[2 * h], 1, 3), widen<STORE>(vf[2 * h + 1], 1, 3));
             }
           }
         } else {
