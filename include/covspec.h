@@ -280,18 +280,20 @@ int covspec_cache_read(const covspec_cache* cache, const covspec_tokens* tokens,
 /* Attention of the call's tokens over the cache, which already holds them (covspec_cache_write).  The token at position p
  * attends to the positions max(0, p - window + 1) .. p of its request: o = sum_j softmax_j(scale q . k_j) v_j.  Query head h
  * reads key head h / (q_heads / heads).  Probabilities are rounded to dtype before the second product; scores, maxima, sums and
- * accumulators are float32.  A token without a key (a position below 0) gets zeros and the sum -inf.  What the cache holds past
- * a request's length is never read; the values of its positions that a token may not see have to be finite where another token
- * of the call may see them.
+ * accumulators are float32.  A token without a key (a position below 0) gets zeros and the sum -inf.  What the pages hold past
+ * a request's length, or before every window of the call, does not matter, whatever it is; the values at positions that one of a
+ * request's new tokens sees and another does not have to be finite, or both may become NaN.
  *  dtype         of q and out: COVSPEC_BF16 or COVSPEC_F16; the cache's store is the same or an 8-bit one
  *  q, out        device [n] rows [q_heads, head_dim], dense, q_stride (out_stride) elements apart; multiples of 16 bytes
  *  q_heads       a multiple of the cache's heads
  *  window        0: none
- *  max_new       most tokens of a request, or 0: unknown.  A hint for the choice of the kernels: results do not depend on it
+ *  max_new       most tokens of a request, or 0: unknown.  A hint for the choice of the kernels, which shows in the last bits
+ *                only; requests with more are answered all the same
  *  lse           device [n, q_heads] float32 or NULL (out): log of the sum of exp(scale q . k_j)
  *  workspace     device, covspec_cache_attend_workspace(...) bytes, 16-byte aligned; contents do not matter.  Calls that may
  *                overlap on the GPU need workspaces of their own
- * Results are deterministic, and how the work was split shows in the last bits only. */
+ * Results are deterministic; how the work was split, which follows the whole batch, shows in the last bits only.  Waits inside the
+ * kernels are bounded; there is no status word here, so one that gives up leaves NaN in the rows at hand. */
 int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
                          long long q_stride, int q_heads, float scale, int window, int max_new, void* out, long long out_stride,
                          float* lse, void* workspace, long long workspace_bytes, void* stream);

@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcovspec.so")
 LIB_DEBUG = os.path.join(HERE, "libcovspec_debug.so")     # the same sources with -DCOVSPEC_DEBUG_BOUNDS
 OBJECTS = os.path.join(HERE, "_build")                    # a compiled source is used again until one of its files changes
-SOURCES = ["covspec.cu", "verify.cu"]
+SOURCES = ["covspec.cu", "verify.cu", "attend_bf16.cu", "attend_f16.cu"]
 BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
 
 

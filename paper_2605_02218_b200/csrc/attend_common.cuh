@@ -85,7 +85,7 @@ struct Cursor {
       if (++h == p.c.heads) {
         h = 0;
         do {
-          if (++b >= p.t.batch) { units = 0x7fffffff; return; }
+          if (++b >= p.t.batch) { units = 0x3fffffff; return; }   // behind the last item
           r = load_request(p, b);
         } while (!r.rows);
       }

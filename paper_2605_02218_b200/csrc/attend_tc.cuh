@@ -13,6 +13,7 @@
 // while a unit's probabilities add up to at most 2^14, so that O is rescaled seldom and one pass over S makes the probabilities.  A
 // warp with a row beyond that goes over S again with new references.
 #pragma once
+#include "attend_call.cuh"
 #include "attend_kernels.cuh"
 
 namespace covspec {
@@ -21,7 +22,7 @@ namespace wide {
 
 using namespace tc;
 
-constexpr int kRows = 256, kKeys = 128;
+constexpr int kRows = kWideRows, kKeys = kWideKeys;
 constexpr int kThreads = 20 * 32, kSoftmaxWarps = 16;
 constexpr int kCopyWarps = 3, kProducers = kCopyWarps * 32;
 constexpr int kOpen = 4;                    // units that beginning and ending an item costs (8 prompts of 2048 tokens: 688 us without, 604)

@@ -3,6 +3,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <string>
 
 namespace covspec {
@@ -63,6 +64,21 @@ inline EncodeTiledFn encode_tiled_fn() {
     return reinterpret_cast<EncodeTiledFn>(ptr);
   }();
   return fn;
+}
+
+// Once for each device: the kernel's limit of dynamic shared memory.
+template <auto Kernel>
+cudaError_t allow_shared(int bytes) {
+  static std::atomic<unsigned long long> configured{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1ull)) {
+    e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
+  }
+  return cudaSuccess;
 }
 
 }  // namespace covspec

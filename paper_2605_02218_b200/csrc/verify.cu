@@ -7,8 +7,7 @@
 #include <algorithm>
 #include <atomic>
 
-#include "attend_kernels.cuh"
-#include "attend_tc.cuh"
+#include "attend_call.cuh"
 #include "host.cuh"
 #include "logits_kernels.cuh"
 
@@ -19,21 +18,6 @@ namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 int bytes_of(int dtype) { return dtype == COVSPEC_F32 ? 4 : dtype == COVSPEC_BF16 || dtype == COVSPEC_F16 ? 2 : 1; }
 bool is_dtype(int dtype) { return dtype == COVSPEC_F32 || dtype == COVSPEC_BF16 || dtype == COVSPEC_F16; }
-
-// Once for each device: the kernel's limit of dynamic shared memory.
-template <auto Kernel>
-cudaError_t allow_shared(int bytes) {
-  static std::atomic<unsigned long long> configured{0};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev >= 64 || !(configured.load(std::memory_order_acquire) >> dev & 1ull)) {
-    e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
-  }
-  return cudaSuccess;
-}
 
 int check_cache(const covspec_cache* c) {
   if (!c || !c->k || !c->v) return COVSPEC_ERR_ARG;
@@ -99,58 +83,7 @@ int cache_grid(int rows, int lanes, int passes) {
   return (int)(((long long)rows + per - 1) / per);
 }
 
-// Largest request, as rows of a key head, that the attention kernel for few rows takes when both run; its CTAs at most per SM.
-constexpr int kFewRows = 64, kRowsCtas = 2;
 long long part_bytes(int ctas, int rows, int dim) { return 2ll * ctas * rows * (dim + 2) * 4; }
-
-// The keys or the values of a cache as [pages, heads * page_size, dim]: boxes of a page's rows of one head, at most `keys`, 128 bytes
-// wide (64 where a row has no more), in tiles with the swizzle of that width.
-bool make_page_map(CUtensorMap* map, const covspec_cache* c, const void* base, long long page_stride, int keys) {
-  EncodeTiledFn encode = encode_tiled_fn();
-  if (!encode) {
-    g_cuda_error = "cuTensorMapEncodeTiled is not available";
-    return false;
-  }
-  const int e = bytes_of(c->store);
-  const cuuint64_t dims[3] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->heads * c->page_size, (cuuint64_t)c->pages};
-  const cuuint64_t strides[2] = {(cuuint64_t)c->head_dim * e, (cuuint64_t)page_stride * e};
-  const cuuint32_t width = (cuuint32_t)std::min(c->head_dim * e, 128);
-  const cuuint32_t box[3] = {width / e, (cuuint32_t)std::min(c->page_size, keys), 1}, step[3] = {1, 1, 1};
-  const CUresult r = encode(map, e == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3,
-                            const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) g_cuda_error = "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r);
-  return r == CUDA_SUCCESS;
-}
-
-template <typename T, int STORE, int DIM, int ROWS>
-cudaError_t launch_rows(const attend::Params& prm, const covspec_cache* cache, int ctas, cudaStream_t s) {
-  constexpr auto kernel = attend::attend_kernel<T, STORE, DIM, ROWS>;
-  using L = attend::Layout<STORE, DIM, ROWS>;
-  cudaError_t e = allow_shared<kernel>(L::kSmem);
-  if (e != cudaSuccess) return e;
-  CUtensorMap map_k, map_v;
-  if (!make_page_map(&map_k, cache, cache->k, cache->k_page_stride, L::kKeys) || !make_page_map(&map_v, cache, cache->v, cache->v_page_stride, L::kKeys))
-    return cudaErrorInvalidValue;
-  e = launch_dependent(kernel, dim3((unsigned)ctas), attend::kThreads, L::kSmem, s, map_k, map_v, prm);
-  if (e != cudaSuccess) return e;
-  return launch_dependent(attend::attend_join_kernel<T, ROWS, DIM>, dim3((unsigned)ctas, ROWS / 4), 128, 0, s, prm);
-}
-
-template <typename T, int STORE, int DIM>
-cudaError_t launch_wide(const attend::Params& prm, const covspec_cache* cache, int ctas, cudaStream_t s) {
-  constexpr auto kernel = attend::wide::attend_wide_kernel<T, STORE, DIM>;
-  constexpr int smem = attend::wide::Layout<STORE, DIM>::kSmem, rows = attend::wide::kRows;
-  cudaError_t e = allow_shared<kernel>(smem);
-  if (e != cudaSuccess) return e;
-  CUtensorMap map_k{}, map_v{};
-  if (!make_page_map(&map_k, cache, cache->k, cache->k_page_stride, attend::wide::kKeys) || !make_page_map(&map_v, cache, cache->v, cache->v_page_stride, attend::wide::kKeys))
-    return cudaErrorInvalidValue;
-  e = launch_dependent(kernel, dim3((unsigned)ctas), attend::wide::kThreads, smem, s, map_k, map_v, prm);
-  if (e != cudaSuccess) return e;
-  return launch_dependent(attend::attend_join_kernel<T, rows, DIM>, dim3((unsigned)ctas, rows / 4), 128, 0, s, prm);
-}
 
 }  // namespace
 
@@ -218,8 +151,8 @@ long long covspec_cache_attend_workspace(const covspec_cache* cache, int q_heads
   if (q_heads < 1 || q_heads % cache->heads) return COVSPEC_ERR_SHAPE;
   int sms = 0;
   if (const int e = sm_count(&sms)) return e;
-  return part_bytes(kRowsCtas * sms, kFewRows, cache->head_dim) + part_bytes(sms, attend::wide::kRows, cache->head_dim) +
-         32ll * (kRowsCtas + 1) * sms;
+  return part_bytes(attend::kRowsCtas * sms, attend::kFewRows, cache->head_dim) + part_bytes(sms, attend::kWideRows, cache->head_dim) +
+         32ll * (attend::kRowsCtas + 1) * sms;
 }
 
 int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
@@ -254,43 +187,26 @@ int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* token
   prm.rows_over = 0; prm.rows_upto = INT_MAX;
   prm.least_units = 1;
   prm.open = static_cast<int4*>(workspace);
-  prm.part = reinterpret_cast<float*>(prm.open + 2ll * (kRowsCtas + 1) * sms);
+  prm.part = reinterpret_cast<float*>(prm.open + 2ll * (attend::kRowsCtas + 1) * sms);
   // rows of a key head in the largest request.  Where some may have many, each of the two kernels takes its requests
   const long long most = (long long)(max_new > 0 ? std::min(max_new, n) : n) * prm.group;
   const int rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
-  const bool both = most > kFewRows && cache->store < COVSPEC_E4M3;
+  const bool both = most > attend::kFewRows && cache->store < COVSPEC_E4M3;
   // no more CTAs than there can be units
   auto ctas_of = [&](int rows, int keys, int ctas) {
     const long long items = ((long long)n * prm.group / rows + prm.t.batch) * cache->heads;
     return (int)std::min<long long>(ctas, items * (((long long)prm.t.width * cache->page_size + keys - 1) / keys + 1));
   };
-  const int ctas = ctas_of(rows, 64, kRowsCtas * sms);
+  const int ctas = ctas_of(rows, 64, attend::kRowsCtas * sms);
   attend::Params wide = prm;
-  wide.rows_over = kFewRows;
-  wide.open = prm.open + 2ll * kRowsCtas * sms;
-  wide.part = prm.part + part_bytes(kRowsCtas * sms, kFewRows, cache->head_dim) / 4;
-  const int wide_ctas = ctas_of(attend::wide::kRows, attend::wide::kKeys, sms);
-  if (both) prm.rows_upto = kFewRows;
+  wide.rows_over = attend::kFewRows;
+  wide.open = prm.open + 2ll * attend::kRowsCtas * sms;
+  wide.part = prm.part + part_bytes(attend::kRowsCtas * sms, attend::kFewRows, cache->head_dim) / 4;
+  const int wide_ctas = ctas_of(attend::kWideRows, attend::kWideKeys, sms);
+  if (both) prm.rows_upto = attend::kFewRows;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  auto of_type = [&](auto* tag) {
-    using T = std::remove_pointer_t<decltype(tag)>;
-    constexpr int kOwn = std::is_same_v<T, __half> ? cache::kF16 : cache::kBF16;
-    return with_dim(cache->head_dim, [&](auto dim) {
-      constexpr int kDim = decltype(dim)::value;
-      auto of_store = [&](auto store) {
-        constexpr int kStore = decltype(store)::value;
-        if constexpr (kStore < cache::kE4M3) {
-          if (both)
-            if (const cudaError_t e = launch_wide<T, kStore, kDim>(wide, cache, wide_ctas, s); e != cudaSuccess) return e;
-        }
-        return rows == 16 ? launch_rows<T, kStore, kDim, 16>(prm, cache, ctas, s)
-               : rows == 32 ? launch_rows<T, kStore, kDim, 32>(prm, cache, ctas, s) : launch_rows<T, kStore, kDim, 64>(prm, cache, ctas, s);
-      };
-      return cache->store == COVSPEC_E4M3 ? of_store(Const<cache::kE4M3>())
-             : cache->store == COVSPEC_INT8 ? of_store(Const<cache::kInt8>()) : of_store(Const<kOwn>());
-    });
-  };
-  CUDA_TRY(dtype == COVSPEC_BF16 ? of_type((__nv_bfloat16*)nullptr) : of_type((__half*)nullptr));
+  const attend::Call call{prm, wide, cache, rows, ctas, both ? wide_ctas : 0, s};
+  CUDA_TRY(dtype == COVSPEC_BF16 ? attend::launch_bf16(call) : attend::launch_f16(call));
   return COVSPEC_OK;
 }
 
@@ -315,7 +231,8 @@ int covspec_edit_logits(int logit_dtype, int rows, int vocab, long long ld, cons
   int sms = 0;
   if (const int st = sm_count(&sms)) return st;
   // Rows of a CTA share the tables of their request, which cost a pass over the history; segments of 4096 entries and groups of
-  // rows as long as two CTAs an SM are left, then smaller ones (8 rows x 151674: see the design notes).
+  // rows (of one block mostly) as long as four CTAs an SM are left, smaller segments where there are not two (1024 rows x 151674,
+  // groups of 16 / 8 / 4: 188 / 172 / 203 us).
   prm.segment = 4096;
   prm.group = 1;
   auto segments_of = [&] { return (unsigned)((vocab + prm.segment - 1) / prm.segment); };

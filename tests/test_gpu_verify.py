@@ -647,6 +647,40 @@ def test_the_binding_refuses_memory_that_the_kernels_must_not_touch():
         api.edit_logits(z[:, ::2], prefix([3]))
 
 
+def test_without_the_native_part_the_calls_give_the_same(monkeypatch):
+    states = [verify_state(s, store) for s, store in ((60, "e4m3"), (61, "bf16"))]
+    def calls():
+        got = []
+        for s in states:
+            got += list(verify_step(s)) + list(s["p"].cache.read(*s["t"], len(s["u"]), dtype=torch.float16))
+            got += list(s["p"].cache.attend(s["q"], *s["t"], window=7, lse=True))
+        return got
+    want = [x.clone() for x in calls()]
+    monkeypatch.setattr(api, "_native", None)
+    assert all(torch.equal(a, b) for a, b in zip(want, calls()))
+
+
+def test_prompts_and_steps_of_many_requests_in_one_call():
+    # both kernels share the call; several items a share, the ring round many times
+    rng = np.random.default_rng(12)
+    length = [int(v) for v in rng.integers(200, 1500, 12)]
+    new = [int(min(v, rng.choice([1, 4, 40, 300]))) for v in length]
+    for store, dtype in (("bf16", torch.bfloat16), ("f16", torch.float16), ("int8", torch.float16)):
+        p = Paged(62, store, 2, 64, 32, new, length)
+        g = torch.Generator(device=DEV).manual_seed(3)
+        q = torch.randn(sum(new), 14, 64, generator=g, device=DEV).to(dtype)
+        first, lse = p.cache.attend(q, *p.tokens(), window=256, lse=True)
+        for _ in range(300):                                     # calls back to back
+            got, l = p.cache.attend(q, *p.tokens(), window=256, lse=True)
+        assert torch.equal(got, first) and torch.equal(l, lse)
+        keep = [b for b, m in enumerate(new) if m <= 4]          # the oracle is slow: the short ones, row by row
+        at = np.concatenate([[0], np.cumsum(new)])
+        for b in keep:
+            small = Paged.__new__(Paged)
+            small.__dict__.update(p.__dict__, new=[0] * b + [new[b]] + [0] * (len(new) - b - 1))
+            attend_check(small, q[at[b]:at[b + 1]], first[at[b]:at[b + 1]], lse[at[b]:at[b + 1]], 0.125, 256)
+
+
 def test_empty_calls():
     p = Paged(52, "bf16", 2, 64, 16, [0, 0], [20, 30])
     e = torch.empty(0, 2, 64, dtype=torch.bfloat16, device=DEV)
