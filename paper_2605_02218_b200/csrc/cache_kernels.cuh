@@ -6,6 +6,9 @@
 // 8-bit form of a row x: scale = max(max|x| / L, 2^-100) in float32, L = 448 (e4m3) or 127; held = x / scale, rounded once,
 // half to even, from the exact quotient.  The bound on the scale keeps the quotients normal numbers; a row with a value that
 // is not finite gets the scale NaN and so reads back as NaN.
+//
+// Both directions are bound by HBM when they are large.  27.8 k kept tokens x 8 heads x 128 from bf16 to int8: 49 us, 3.5 TB/s (the
+// quantising arithmetic, about 13 instructions a value, is not hidden entirely); e4m3 back to bf16, 146 k tokens: 155-160 us, 5.7 TB/s.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
