@@ -8,8 +8,8 @@
 // unit to unit each at its own pace and meet at the end of an item only.
 //
 // Measured (reading the cache once is the floor): 64 single tokens over e4m3 caches of 500-16384 positions, 32 query heads on 8 of 128:
-// 137 us, 4.2 TB/s; blocks of 8 tokens over 32 bf16 caches of 300-4096, 28 heads on 4: 44 us, 2.0 TB/s; 24 prompt chunks of up to 700
-// tokens over int8 caches, 14 heads on 2 of 64, window 1024: 312 us.  Bound by the chain of instructions of a warp from unit to unit
+// 142 us, 4.1 TB/s; blocks of 8 tokens over 32 bf16 caches of 300-4096, 28 heads on 4: 44 us, 2.0 TB/s; 24 prompt chunks of up to 700
+// tokens over int8 caches, 14 heads on 2 of 64, window 1024: 326 us.  Bound by the chain of instructions of a warp from unit to unit
 // (eight computing warps an SM; issue slots 42 % busy, HBM 36 % in the first of these at 200 us), the last one by mma.sync's rate.
 //
 // 8-bit rows are exact in float16, so their scales stay outside the products: s_ij = (q_i . k_j) * key scale, and the probability
@@ -60,9 +60,9 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// The exponent of a positive number: near enough to its logarithm for a reference.
+// The exponent of a number that is not negative, 0 for NaN: near enough to its logarithm for a reference.
 __device__ __forceinline__ float exponent_of(float x) {
-  return __uint_as_float(0x4b000000u | (__float_as_uint(x) >> 23)) - (8388608.f + 127.f);
+  return x == x ? __uint_as_float(0x4b000000u | (__float_as_uint(x) >> 23)) - (8388608.f + 127.f) : 0.f;
 }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -88,7 +88,7 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
 // whatever the type of the queries: both widen to it in fewer instructions than to bfloat16, and probabilities keep three more
 // bits.  Queries in bfloat16 are brought to float16 by a power of two for each row (to_half).
 //  e4m3: the conversion instruction (half of the pairs by shifts and a product with 2^8 instead, exact too: 64 caches of 500-16384
-//        positions, 8 heads of 128, 138 -> 160 us; all of them 189).
+//        positions, 8 heads of 128, 138 -> 160 us; all of K's 189).
 //  int8: the byte becomes the lower bits of 1024 + (v + 128), and 1152 is taken off.
 template <int STORE>
 __device__ __forceinline__ uint32_t widen(uint32_t bytes, int lo, int hi) {

@@ -474,6 +474,21 @@ def test_a_row_that_is_not_finite_reaches_only_its_request():
     assert out[[0] + list(range(2, 22))].isfinite().all()
 
 
+@pytest.mark.parametrize("store", ["e4m3", "int8"])
+def test_a_value_that_is_not_finite_leaves_the_sum(store):
+    # the keys are in order: the rows are NaN, their log-sums are not
+    p = Paged(33, store, 1, 128, 16, [1, 2], [300, 40])
+    v = p.v.clone()
+    v[7, 0, 5] = math.inf
+    q = torch.randn(3, 4, 128, device=DEV).half()
+    _, want = p.cache.attend(q, *p.tokens(), lse=True)
+    p.cache.write(p.k, v, prefix(p.length), p.lengths, p.d_table)
+    out, lse = p.cache.attend(q, *p.tokens(), lse=True)
+    assert out[0].isnan().all() and out[1:].isfinite().all()
+    # the reference moves by one key's exponent at most: float32 sums of 300 positive numbers, 2^-23 each
+    assert ((lse - want).abs() <= 364 * 2.0 ** -23 + 2.0 ** -22 * want.abs()).all()
+
+
 def test_rows_strides_and_outputs_of_the_callers_own():
     p = Paged(31, "bf16", 2, 128, 16, [3, 70], [40, 200])
     n = 73
