@@ -98,7 +98,7 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 }
 
 // Barriers among `n` threads.  Not the aligned forms: those want the warp's lanes together, which nothing after a branch on the lane
-// promises; with them a large call of one build stood still.
+// promises.
 __device__ __forceinline__ void meet_at(int id, int n) {
   __syncwarp();
   asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(n) : "memory");
@@ -191,35 +191,12 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   if (warp > kSoftmaxWarps) {
     // ---------------- producers ----------------
     const int wp = warp - kSoftmaxWarps - 1;
-    uint64_t* waiting[3] = {nullptr, nullptr, nullptr};        // barriers of copies that are under way, the oldest last
-    auto close = [&](uint64_t* bar) {                          // the copies so far belong to `bar`
-      copies_close();
-      if (waiting[2]) { copies_wait<3>(); fence_async_proxy(); mbar_arrive(waiting[2]); }
-      waiting[2] = waiting[1];
-      waiting[1] = waiting[0];
-      waiting[0] = bar;
-    };
-    auto flush = [&] {
-      copies_wait<0>();
-      fence_async_proxy();
-#pragma unroll
-      for (int i = 2; i >= 0; --i) {
-        if (waiting[i]) mbar_arrive(waiting[i]);
-        waiting[i] = nullptr;
-      }
-    };
-    // nothing is waited for while copies that the others may need to get on have not been handed over
-    auto acquire = [&](uint64_t* bar, uint32_t parity) {
-      if (__all_sync(0xffffffffu, mbar_peek(bar, parity))) return true;
-      flush();
-      return warp_wait(bar, parity, abort_flag);
-    };
     int slot = 0;
     uint32_t phase = 1, q_phase = 1;
     bool ok = true, fresh = true;
     auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
     auto queries = [&] {                                       // of the item at `at`
-      ok = ok && acquire(q_empty, q_phase);
+      ok = ok && warp_wait(q_empty, q_phase, abort_flag);
       q_phase ^= 1u;
       constexpr int kChunks = DIM / 8, kAtOnce = 32 / kChunks, kStep = kCopyWarps * kAtOnce;
       const int chunk = lane % kChunks;
@@ -238,15 +215,15 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         uint8_t* to = smem + (row >> 7) * (128 * DIM * 2) + tile_at(128, row & 127, chunk);
         if (in) copy16(smem_u32(to), q, is);
       }
-      close(q_full);
+      copies_close();
+      copies_wait<0>();
+      fence_async_proxy();
+      mbar_arrive(q_full);
     };
     {
       if (wp > 0) {                                            // these two only help with the queries
         for (int u = 0; u < count && ok; ++u) {
-          if (fresh) {
-            queries();
-            flush();
-          }
+          if (fresh) queries();
           fresh = at.unit + 1 == at.units;
           if (u + 1 < count) at.next(p);
         }
@@ -266,7 +243,6 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           const bool begins = fresh;
           if (begins) {
             queries();
-            flush();
             whole_start = at.unit == 0;
           }
           const int row0 = at.tile * kRows, key0 = at.key, page_row = (at.h << p.c.page_shift) + ((key0 + (box << shift)) & mask);
