@@ -231,7 +231,8 @@ int covspec_correct(int logit_dtype, int rows, int vocab, long long ld, const vo
  * scale for each position and head, [pages, heads, page_size] dense.  A row x is held as x / scale, rounded once, half to even,
  * from the exact quotient, with scale = max(max|x| / L, 2^-100) in float32 and L = 448 or 127.  A row with a value that is not
  * finite gets the scale NaN, which makes everything that reads it NaN.  The codes of NaN (e4m3) and -128 (int8) are not
- * written; a cache from elsewhere must not hold the former, and its scales must not be negative. */
+ * written; a cache from elsewhere must not hold the former, and its scales must not be negative.  Scales below 2^-100, 0 among
+ * them, are scales like others in the softmax and its sums; the values themselves, below 2^-91 then, may count as zeros. */
 #define COVSPEC_E4M3 3
 #define COVSPEC_INT8 4
 typedef struct {

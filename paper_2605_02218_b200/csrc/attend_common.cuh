@@ -220,8 +220,11 @@ __global__ void __launch_bounds__(128) attend_join_kernel(Params p) {
 #pragma unroll 4
   for (int s = share; s <= more.x; ++s) {
     const float* slot = slot_of(s);
-    const float w = exp2f(slot[ROWS * DIM + row] - safe);
-    sum += w * slot[ROWS * (DIM + 1) + row];
+    // in two steps: sums of 8-bit caches go on counting where the references are more than 2^126 apart
+    const float apart = slot[ROWS * DIM + row] - safe, near = fmaxf(apart, -120.f), rest = exp2f(apart - near);
+    float w = exp2f(near);
+    sum += w * (slot[ROWS * (DIM + 1) + row] * rest);
+    w *= rest;
     const float* x = slot + row * DIM + lane * kPer;
     if constexpr (kPer == 4) {
       const float4 v = *reinterpret_cast<const float4*>(x);

@@ -14,7 +14,8 @@
 //
 // 8-bit rows are exact in float16, so their scales stay outside the products: s_ij = (q_i . k_j) * key scale, and the probability
 // takes the value's scale before it is rounded to 16 bits.  So that it cannot leave float16's range, the running maximum is the
-// one of s_ij + the exponent of the value's scale.
+// one of s_ij + lift_of(value's scale), whatever the scales are; sums of the probabilities alone may then be as large as 2^93 a key
+// (rows of zeros) or as small as 2^-108, and go to a new reference in two steps.
 #pragma once
 #include <type_traits>
 
@@ -60,9 +61,11 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// The exponent of a number that is not negative, 0 for NaN: near enough to its logarithm for a reference.
-__device__ __forceinline__ float exponent_of(float x) {
-  return x == x ? __uint_as_float(0x4b000000u | (__float_as_uint(x) >> 23)) - (8388608.f + 127.f) : 0.f;
+// What a value's scale (not negative) adds to the reference: its exponent, near enough to its logarithm, less 13.  A probability times
+// its scale is below 2^14 then, and float16 holds it in full down to 2^-27 of the row's largest.  No less than -80 for the exponent (also
+// for NaN), so that the sum of 2^30 keys with values of zero stays finite; scales down to 2^-100 still give normal numbers.
+__device__ __forceinline__ float lift_of(float x) {
+  return __uint_as_float(0x4b000000u | (__float_as_uint(fmaxf(x, 8.271806125530277e-25f)) >> 23)) - (8388608.f + 127.f + 13.f);
 }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -363,7 +366,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             by[i] = sc[j * 8 + 2 * tq + i];
-            lift[i] = exponent_of(sc[kKeys + j * 8 + 2 * tq + i]);
+            lift[i] = lift_of(sc[kKeys + j * 8 + 2 * tq + i]);
           }
         }
 #pragma unroll
@@ -384,9 +387,15 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 1));
         best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 2));
         safe[i] = best[i] == -INFINITY ? 0.f : best[i];
-        shrink[i] = ex2(top[i] - safe[i]);
+        if constexpr (k8) {                                      // a reference may rise by more than 2^126
+          const float part = ex2(0.5f * (top[i] - safe[i]));
+          shrink[i] = part * part;
+          sum[i] = sum[i] * part * part;
+        } else {
+          shrink[i] = ex2(top[i] - safe[i]);
+          sum[i] *= shrink[i];
+        }
         top[i] = best[i];
-        sum[i] *= shrink[i];
       }
       if (__any_sync(0xffffffffu, shrink[0] != 1.f || shrink[1] != 1.f)) {
 #pragma unroll
@@ -463,9 +472,16 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
               const float* x = box + (g + 8 * i) * DIM;
               const float2 ts = box_ts[which * 16 + g + 8 * i];
               const float both = fmaxf(top[i], ts.x), ref = both == -INFINITY ? 0.f : both;
-              const float a = ex2(top[i] - ref), c = ex2(ts.x - ref);
+              constexpr float kHalf = k8 ? 0.5f : 1.f;
+              float a = ex2(kHalf * (top[i] - ref)), c = ex2(kHalf * (ts.x - ref));
               top[i] = both;
-              sum[i] = sum[i] * a + ts.y * c;
+              if constexpr (k8) {
+                sum[i] = sum[i] * a * a + ts.y * c * c;
+                a *= a;
+                c *= c;
+              } else {
+                sum[i] = sum[i] * a + ts.y * c;
+              }
 #pragma unroll
               for (int j = 0; j < DIM / 8; ++j) {
                 const float2 v = *reinterpret_cast<const float2*>(x + ((j ^ g) * 8 + 2 * tq));
