@@ -251,7 +251,8 @@ typedef struct {
  * ones of its lengths[b] positions (token i of n has position lengths[b] - n + i).  Position t lies in page
  * table[b * table_stride + t / page_size].  Positions below 0 or past the table, and page ids outside the cache, have no place:
  * nothing is written there, zeros are read back, and their keys are not attended to.  Tokens of no request (before offsets[0],
- * from offsets[batch] on) are left alone, and so are the outputs' rows of them. */
+ * from offsets[batch] on) are left alone, and so are the outputs' rows of them; of a request that reaches past the call's n tokens
+ * the others keep their positions. */
 typedef struct {
   int batch;
   const int* offsets;          /* device [batch + 1], ascending                                    */

@@ -34,17 +34,18 @@ struct Params {
 
 // One request as the kernels see it.  Offsets, lengths and positions that make no sense give it no rows or no keys.
 struct Request {
-  int q0, n, length, keys, rows;
+  int q0, first, keys, rows;     // first token; its position
 };
 __device__ __forceinline__ Request load_request(const Params& p, int b) {
   Request r;
   const int a = p.t.offsets[b], e = p.t.offsets[b + 1];
+  const int length = max(p.t.lengths[b], 0);
   r.q0 = max(a, 0);
-  r.n = max(min(e, p.n) - r.q0, 0);
-  r.length = max(p.t.lengths[b], 0);
-  // positions count from the call's own tokens: the ones in front of a cut-off start keep theirs
-  r.keys = (int)min((long long)r.length, (long long)p.t.width << p.c.page_shift);
-  r.rows = r.n * p.group;
+  // a token keeps its position where its request begins before the call's rows or ends behind them; a call has fewer than 2^30 tokens,
+  // so what lies further below 0 stays there
+  r.first = max(length - max(e - r.q0, 0), -(1 << 30));
+  r.keys = (int)min((long long)length, (long long)p.t.width << p.c.page_shift);
+  r.rows = max(min(e, p.n) - r.q0, 0) * p.group;
   if (r.rows <= p.rows_over || r.rows > p.rows_upto) r.rows = 0;
   return r;
 }
@@ -52,10 +53,10 @@ struct Range { int lo, hi; };    // keys lo .. hi - 1
 template <int ROWS>
 __device__ __forceinline__ Range keys_of(const Params& p, const Request& r, int tile) {
   const int first = tile * ROWS / p.group, last = min((tile + 1) * ROWS, r.rows) - 1;
-  const int end = r.length - r.n + last / p.group + 1;
+  const int end = r.first + last / p.group + 1;
   Range k;
   k.hi = min(max(end, 0), r.keys);
-  k.lo = p.window ? max(r.length - r.n + first - p.window + 1, 0) : 0;
+  k.lo = p.window ? max(r.first + first - p.window + 1, 0) : 0;
   return k;
 }
 template <int KEYS>

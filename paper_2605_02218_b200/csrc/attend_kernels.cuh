@@ -200,7 +200,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
       const int key0 = at.key, row0 = at.tile * ROWS;
       const bool ends = at.unit + 1 == at.units;
       const int4 say0 = make_int4(key0, (fresh ? kBegins : 0) | (ends ? kEnds : 0) | (whole_start ? kWholeStart : 0), at.r.q0, at.h);
-      const int4 say1 = make_int4(row0, at.r.rows, at.r.length - at.r.n, at.units - 1 - at.unit);
+      const int4 say1 = make_int4(row0, at.r.rows, at.r.first, at.units - 1 - at.unit);
       fresh = ends;
       const int page_row = (at.h << p.c.page_shift) + ((key0 + (box << shift)) & mask), box_page = page;
       uint32_t word[kKeys / 32], all = 0xffffffffu;

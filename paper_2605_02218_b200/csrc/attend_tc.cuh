@@ -248,7 +248,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           const int row0 = at.tile * kRows, key0 = at.key, page_row = (at.h << p.c.page_shift) + ((key0 + (box << shift)) & mask);
           fresh = at.unit + 1 == at.units;
           const int4 item[2] = {make_int4(key0, (begins ? kBegins : 0) | (fresh ? kEnds : 0) | (at.r.rows - row0 > 128 ? kTwo : 0) | (whole_start ? kWholeStart : 0), at.r.q0, at.h),
-                                make_int4(row0, at.r.rows, at.r.length - at.r.n, at.units - 1 - at.unit)};
+                                make_int4(row0, at.r.rows, at.r.first, at.units - 1 - at.unit)};
           const bool mine = page >= 0 && part < DIM / 64;
           const int box_page = page;
           uint32_t word[4];

@@ -1,5 +1,5 @@
-"""The attention over the paged cache where value scales are of very different size.  All rows are held against the definition in 64
-bits, on the GPU."""
+"""The attention over the paged cache where value scales are of very different size and where offsets reach past the call's rows.
+All rows are held against the definition in 64 bits, on the GPU."""
 import math
 
 import numpy as np
@@ -109,3 +109,25 @@ def test_zero_rows_whose_keys_win_by_little(store):
     out, lse = p.cache.attend(q, prefix([2] * n), i32([300] * n), p.d_table.expand(n, -1).contiguous(), scale=1.0, lse=True)
     for i in range(0, 2 * n, 26):
         check(p, q[i:i + 2], out[i:i + 2], lse[i:i + 2], 1.0)
+
+
+# ---- offsets that reach past the call's rows ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("store,dtype", [("bf16", "bf16"), ("e4m3", "f16")])
+@pytest.mark.parametrize("new,n,window", [([3, 6], 7, 0), ([100, 200], 250, 64), ([5, 4, 3], 5, 0)])
+def test_a_token_keeps_its_position_where_the_rows_end_before_the_offsets(store, dtype, new, n, window):
+    p = Paged(81, store, 2, 64, 16, new, [m + 50 for m in new])
+    q = torch.randn(n, 4, 64, device=DEV).to(TYPES[dtype])
+    out, lse = p.cache.attend(q, *p.tokens(), window=window, lse=True)
+    check(p, q, out, lse, 0.125, window)
+
+
+@pytest.mark.parametrize("window", [0, 5, 2 ** 31 - 1])
+def test_offsets_that_make_no_sense_give_no_keys(window):
+    # the requests' ends lie so far behind the rows that every token stands before its cache
+    p = Paged(84, "bf16", 2, 64, 16, [3, 100], [60, 200])
+    q = torch.randn(103, 4, 64, device=DEV).bfloat16()
+    out, lse = p.cache.attend(q, i32([0, 3, 2 ** 31 - 1]), p.lengths, p.d_table, window=window, lse=True)
+    assert (out[3:] == 0).all() and (lse[3:] == -math.inf).all()
+    p.new = [3]
+    check(p, q[:3], out[:3], lse[:3], 0.125, window if window < 2 ** 31 - 1 else 0)
