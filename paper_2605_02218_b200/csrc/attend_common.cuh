@@ -32,6 +32,23 @@ struct Params {
                                  // row, rows; last share of the item
 };
 
+// Nothing in these kernels waits for more than what its own CTA has under way.  A wait in vain takes about a second.
+constexpr uint32_t kPolls = 1u << 18;
+
+// A wait of the whole warp: its lanes poll together and leave together.  And every lane itself arrives at the barrier without which the one
+// that it waits for does not complete again, so that no lane can be left behind by two phases, whatever the compiler makes of the
+// warp's convergence: with a loop of its own for each lane, a vote behind it and arrivals by lane 0, lanes left one by one, and in some
+// builds lane 0 went on alone and the others waited for a phase that was over.  (One lane that polls for all: 202 us for 142 with 64 single
+// tokens over e4m3 caches.)
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  for (uint32_t i = 0; i < kPolls; ++i) {
+    if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar, parity))) return true;
+    if ((i & 255u) == 255u && __any_sync(0xffffffffu, *abort_flag)) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+
 // One request as the kernels see it.  Offsets, lengths and positions that make no sense give it no rows or no keys.
 struct Request {
   int q0, first, keys, rows;     // first token; its position

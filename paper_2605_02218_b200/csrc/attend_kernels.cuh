@@ -136,11 +136,6 @@ __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, ui
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(tc::smem_u32(bar)) : "memory");
 }
-// A wait of the whole warp: its lanes leave the polls one by one, and the instructions that follow want them together.  Nothing here
-// waits for more than what its own CTA has under way, so it gives up early.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, tc::mbar_wait_limited(bar, parity, abort_flag, 1u << 18));
-}
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <typename T, int STORE, int DIM, int ROWS>
@@ -164,9 +159,9 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
   __shared__ long long scratch[kThreads / 32 + 4];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < kS; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, kWarps); }
-    mbar_init(partly, 1);
-    mbar_init(met, kWarps);
+    for (int i = 0; i < kS; ++i) { mbar_init(full + i, 32); mbar_init(empty + i, kWarps * 32); }
+    mbar_init(partly, 32);
+    mbar_init(met, kWarps * 32);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -230,6 +225,8 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll
         for (int i = 0; i < kKeys / 32; ++i) there[i] = word[i];
         mbar_expect_tx(bar, bytes);
+      } else {
+        mbar_arrive(bar);
       }
       __syncwarp();
       if (mine) {
@@ -250,8 +247,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             if constexpr (k8) sc[kKeys + 32 * i + lane] = 0.f;
           }
         fence_async_proxy();                                   // before copies into the same place
-        __syncwarp();
-        if (lane == 0) mbar_arrive(full + stage);
+        mbar_arrive(full + stage);
       }
       if (++stage == kS) { stage = 0; phase ^= 1u; }
     }
@@ -275,8 +271,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     bool ok = true, inside = false;   // between an item's first unit and its last
     int q0 = 0, h = 0, tile_row = 0;  // the item at hand
     auto meet = [&] {
-      __syncwarp();
-      if (lane == 0) mbar_arrive(met);
+      mbar_arrive(met);
       ok = warp_wait(met, met_phase, abort_flag) && ok;
       met_phase ^= 1u;
     };
@@ -541,8 +536,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         }
         inside = false;
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(empty + stage);
+      mbar_arrive(empty + stage);
       if (++stage == kS) { stage = 0; phase ^= 1u; }
     }
     if (!ok && inside && wk == 0) {                            // a wait gave up: the item at hand becomes NaN

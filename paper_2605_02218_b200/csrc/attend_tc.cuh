@@ -162,12 +162,12 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
+    for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, 32); mbar_init(empty + i, 1); }
     mbar_init(q_full, kProducers);
     mbar_init(q_empty, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(s_full + i, 1); mbar_init(p_ready + i, 8); mbar_init(o_full + i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(s_full + i, 1); mbar_init(p_ready + i, 8 * 32); mbar_init(o_full + i, 1); }
     mbar_init(drained, 1);
-    mbar_init(partly, 1);
+    mbar_init(partly, 32);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -270,6 +270,8 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             units[(u & 3) * 2] = item[0];
             units[(u & 3) * 2 + 1] = item[1];
             mbar_expect_tx(full + slot, bytes);
+          } else {
+            mbar_arrive(full + slot);
           }
           __syncwarp();
           if (mine) tma_load_3d(smem_u32(ring + slot * L::kSlot) + part * (kKeys * 128) + (box << shift) * 128, &map_k, part * 64, page_row, box_page, full + slot);
@@ -278,6 +280,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           const bool all = (word[0] & word[1] & word[2] & word[3]) == 0xffffffffu;
           uint64_t* bar = all ? full + slot : partly;
           if (lane == 0) mbar_expect_tx(bar, bytes);
+          else mbar_arrive(bar);
           __syncwarp();
           if (mine) tma_load_3d(smem_u32(ring + slot * L::kSlot) + part * (kKeys * 128) + (box << shift) * 128, &map_v, part * 64, page_row, box_page, bar);
           if (!all) {                                          // values of keys that are not there: zeros, whatever memory holds
@@ -290,8 +293,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 for (int c = 0; c < DIM / 8; ++c)
                   *reinterpret_cast<uint4*>(ring + slot * L::kSlot + (c >> 3) * (kKeys * 128) + (32 * i + lane) * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
             fence_async_proxy();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(full + slot);
+            mbar_arrive(full + slot);
           }
           next_slot();
         }
@@ -305,57 +307,51 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
   } else if (warp == kSoftmaxWarps) {
     // ---------------- products ----------------
-    const uint32_t qk = idesc<T>(kKeys, false), pv = idesc<T>(DIM, true);
-    int slot = 0;
-    uint32_t phase = 0, q_phase = 0, p_phase = 0;
-    bool ok = true;
-    auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
-    auto scores = [&](int x, int s) {
-      const uint32_t a0 = smem_u32(smem + x * (128 * DIM * 2)), b0 = smem_u32(ring + s * L::kSlot);
+    if (lane == 0) {
+      const uint32_t qk = idesc<T>(kKeys, false), pv = idesc<T>(DIM, true);
+      int slot = 0;
+      uint32_t phase = 0, q_phase = 0, p_phase = 0;
+      bool ok = true;
+      auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
+      auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = ok && mbar_wait_limited(bar, parity, abort_flag, kPolls); };
+      auto scores = [&](int x, int s) {
+        const uint32_t a0 = smem_u32(smem + x * (128 * DIM * 2)), b0 = smem_u32(ring + s * L::kSlot);
 #pragma unroll
-      for (int h = 0; h < DIM / 64; ++h) {
-        const uint64_t a = umma_desc(a0 + h * 128 * 128), b = umma_desc(b0 + h * kKeys * 128);
+        for (int h = 0; h < DIM / 64; ++h) {
+          const uint64_t a = umma_desc(a0 + h * 128 * 128), b = umma_desc(b0 + h * kKeys * 128);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) umma_bf16(tmem + x * 128, a + 2 * k, b + 2 * k, qk, (h | k) != 0);
-      }
-    };
-    auto rows = [&](int x, int s, bool accumulate) {
-      const uint64_t b = desc_mn(smem_u32(ring + s * L::kSlot));
+          for (int k = 0; k < 4; ++k) umma_bf16(tmem + x * 128, a + 2 * k, b + 2 * k, qk, (h | k) != 0);
+        }
+      };
+      auto rows = [&](int x, int s, bool accumulate) {
+        const uint64_t b = desc_mn(smem_u32(ring + s * L::kSlot));
 #pragma unroll
-      for (int k = 0; k < kKeys / 16; ++k)
-        mma_ts(tmem + kO + x * 128, tmem + x * 128 + 8 * k, b + k * (16 * 128 / 16), pv, accumulate || k != 0);
-    };
-    bool opened = false;                                       // the unit's scores are issued
-    for (int u = 0; u < count && ok; ++u) {
-      if (!opened) {                                           // it begins an item here
-        ok = warp_wait(q_full, q_phase, abort_flag);
-        q_phase ^= 1u;
-        ok = ok && warp_wait(full + slot, phase, abort_flag);
-        if (!ok) break;
-        tc_fence_after();
-        if (lane == 0) {
+        for (int k = 0; k < kKeys / 16; ++k)
+          mma_ts(tmem + kO + x * 128, tmem + x * 128 + 8 * k, b + k * (16 * 128 / 16), pv, accumulate || k != 0);
+      };
+      bool opened = false;                                     // the unit's scores are issued
+      for (int u = 0; u < count && ok; ++u) {
+        if (!opened) {                                         // it begins an item here
+          if (!wait(q_full, q_phase) || !wait(full + slot, phase)) break;
+          q_phase ^= 1u;
+          tc_fence_after();
           scores(0, slot);
           umma_commit(s_full);
           if (units[(u & 3) * 2].y & kTwo) scores(1, slot);
           umma_commit(s_full + 1);                             // also without rows: the warps of the tile go from unit to unit
           umma_commit(empty + slot);
+          next_slot();
         }
+        const int flags = units[(u & 3) * 2].y;
+        const bool two = flags & kTwo, more = u + 1 < count && !(flags & kEnds);
+        if (!more) umma_commit(q_empty);
+        const int v_slot = slot;
+        if (!wait(full + v_slot, phase)) break;
         next_slot();
-      }
-      const int flags = units[(u & 3) * 2].y;
-      const bool two = flags & kTwo, more = u + 1 < count && !(flags & kEnds);
-      if (!more && lane == 0) umma_commit(q_empty);
-      const int v_slot = slot;
-      ok = warp_wait(full + v_slot, phase, abort_flag);
-      if (!ok) break;
-      next_slot();
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        ok = ok && warp_wait(p_ready + x, p_phase, abort_flag);
-        if (x == 0 && more) ok = ok && warp_wait(full + slot, phase, abort_flag);
-        if (!ok) break;
-        tc_fence_after();
-        if (lane == 0) {
+        for (int x = 0; x < 2; ++x) {
+          if (!wait(p_ready + x, p_phase) || (x == 0 && more && !wait(full + slot, phase))) break;
+          tc_fence_after();
           if (x == 0 || two) {
             rows(x, v_slot, !(flags & kBegins));
             if (!more) umma_commit(o_full + x);
@@ -366,20 +362,18 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             umma_commit(s_full + x);
           }
         }
-        __syncwarp();
+        p_phase ^= 1u;
+        if (more && ok) {
+          umma_commit(empty + slot);
+          next_slot();
+        }
+        opened = more;
       }
-      p_phase ^= 1u;
-      if (more && ok) {
-        if (lane == 0) umma_commit(empty + slot);
-        next_slot();
-      }
-      opened = more;
-      __syncwarp();
+      // TMEM and the ring are free when every product has ended, also after a wait that gave up
+      umma_commit(drained);
+      volatile int gave_up = 0;
+      mbar_wait_limited(drained, 0, &gave_up, kPolls);
     }
-    // TMEM and the ring are free when every product has ended, also after a wait that gave up
-    if (lane == 0) umma_commit(drained);
-    volatile int gave_up = 0;
-    warp_wait(drained, 0, &gave_up);
     __syncwarp();
   } else {
     // ---------------- softmax ----------------
@@ -418,8 +412,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         sum = 0.f;
       }
       if (!active) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready + x);
+        mbar_arrive(p_ready + x);
       } else {
         const uint4 bits = *reinterpret_cast<const uint4*>(there + (u & 3) * 4);
         // every row of the warp sees all keys of the unit
@@ -509,8 +502,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         tmem_st32(s_at + 32 * half, packed);
         tmem_st_wait();
         tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready + x);
+        mbar_arrive(p_ready + x);
       }
       if ((flags & kEnds) || u + 1 == count) {
         const int4 item = units[(u & 3) * 2 + 1];

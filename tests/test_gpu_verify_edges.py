@@ -131,3 +131,23 @@ def test_offsets_that_make_no_sense_give_no_keys(window):
     assert (out[3:] == 0).all() and (lse[3:] == -math.inf).all()
     p.new = [3]
     check(p, q[:3], out[:3], lse[:3], 0.125, window if window < 2 ** 31 - 1 else 0)
+
+
+# ---- no wait in vain ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,length,heads,group,dim", [([30], [20011], 2, 4, 128), ([20] * 40, [2000] * 40, 4, 4, 64), ([40] * 6, [3001] * 6, 4, 7, 128),
+                                                        ([17, 70, 20, 128] * 8, [1500] * 32, 2, 4, 128)])
+def test_blocks_with_a_tile_and_without_a_second_one(dtype, new, length, heads, group, dim):
+    # items of at most 128 rows, several units and items a block: the second tile's warps only go along.  A wait that has missed its phase
+    # takes 16 ms or more, a call like these 0.1 ms
+    p = Paged(87, dtype, heads, dim, 64, new, length)
+    q = torch.randn(sum(new), heads * group, dim, device=DEV).to(TYPES[dtype])
+    out, lse = p.cache.attend(q, *p.tokens(), lse=True)
+    check(p, q, out, lse, dim ** -0.5)
+    times = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    times[0].record()
+    got = [p.cache.attend(q, *p.tokens()) for _ in range(50)]
+    times[1].record()
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, out) for g in got) and times[0].elapsed_time(times[1]) < 50 * 5
