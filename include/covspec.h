@@ -295,7 +295,8 @@ int covspec_cache_read(const covspec_cache* cache, const covspec_tokens* tokens,
  *  workspace     device, covspec_cache_attend_workspace(...) bytes, 16-byte aligned; contents do not matter.  Calls that may
  *                overlap on the GPU need workspaces of their own
  * Results are deterministic; how the work was split, which follows the whole batch, shows in the last bits only.  Waits inside the
- * kernels are bounded; there is no status word here, so one that gives up leaves NaN in the rows at hand. */
+ * kernels are bounded.  There is no status word here: a block in which one gives up leaves NaN in all rows, and their log-sums, that
+ * it had a part of. */
 int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
                          long long q_stride, int q_heads, float scale, int window, int max_new, void* out, long long out_stride,
                          float* lse, void* workspace, long long workspace_bytes, void* stream);
@@ -427,6 +428,15 @@ int covspec_query_score_static(int dtype, int d, int batch, const void* X, const
  * status word; every score is NaN instead.  Nothing waits and no copy is in flight when it ends. */
 int covspec_selftest_static_timeout(int d, int batch, const void* X, const int* vis_offsets,
                                     const void* Q, const int* txt_offsets, float* s_query, void* stream);
+
+/* Self-test of covspec_cache_attend, with the same arguments.  block < 0: the call with waits that give up at once; every row is NaN.
+ * block >= 0: in that block of each kernel the warp that loads leaves before unit `unit` of the block's share, so that the others wait
+ * in vain; the rows that the block had a part of are NaN.  The limit is a sixteenth of the ordinary one (which is
+ * about a second), and no copy is in flight when it ends. */
+int covspec_selftest_attend_timeout(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
+                                    long long q_stride, int q_heads, float scale, int window, int max_new, void* out,
+                                    long long out_stride, float* lse, void* workspace, long long workspace_bytes, int block, int unit,
+                                    void* stream);
 
 /* Number of kernels the last call on this context launched. */
 int covspec_last_launch_count(const covspec_ctx* ctx);

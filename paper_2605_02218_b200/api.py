@@ -36,7 +36,7 @@ EXPORTS = [
     "covspec_draft_length", "covspec_get_iteration_counts", "covspec_build_has_bounds_checks",
     "covspec_selftest_fill_workspace", "covspec_selftest_static_timeout",
     "covspec_cache_write", "covspec_cache_read", "covspec_cache_attend", "covspec_cache_attend_workspace",
-    "covspec_edit_logits",
+    "covspec_edit_logits", "covspec_selftest_attend_timeout",
 ]
 STATIC_MAX_BATCH = 256
 STATIC_MAX_QUERY_ELEMS = 1 << 20
@@ -161,6 +161,7 @@ def load_library():
     lib.covspec_cache_read.argtypes = [cp, tp, C.c_int, C.c_int, vp, vp, vp]
     lib.covspec_cache_attend.argtypes = [cp, tp, C.c_int, C.c_int, vp, ll, C.c_int, C.c_float, C.c_int, C.c_int, vp, ll, vp, vp,
                                          ll, vp]
+    lib.covspec_selftest_attend_timeout.argtypes = lib.covspec_cache_attend.argtypes[:-1] + [C.c_int, C.c_int, vp]
     lib.covspec_cache_attend_workspace.argtypes = [cp, C.c_int]
     lib.covspec_cache_attend_workspace.restype = ll
     lib.covspec_edit_logits.argtypes = [C.c_int, C.c_int, C.c_int, ll, vp, vp, C.POINTER(Edits), vp]

@@ -7,6 +7,10 @@
 // split follows the lengths on the device and needs no plan from the host.  An item that lies in one share is finished there.
 // The others leave their running maxima, sums and unnormalised rows in the workspace, and attend_join_kernel adds them up in the
 // order of the shares.
+//
+// A block one of whose waits gave up marks its share in `open` and leaves; what it has written by then does not matter.  The join makes
+// every item that has a unit in such a share NaN: the block that joins an item looks at the marks of all its shares, and a marked
+// share's own block goes through the items that begin there.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -29,9 +33,10 @@ struct Params {
   int least_units;               // a share is no smaller
   float* part;                   // [2 * grid][tile_rows * (dim + 2)]: rows, maxima, sums of the shares' first and last item
   int4* open;                    // [grid][2]: the item that a share leaves unfinished: first token of its request, head, first
-                                 // row, rows; last share of the item
+                                 // row, rows; last share of the item, 1 where a wait gave up
+  uint32_t polls;                // that a wait makes before it gives up
+  int stop_share, stop_unit;     // self-test: the loading warp of this share (-1: none) leaves before this unit
 };
-
 // Nothing in these kernels waits for more than what its own CTA has under way.  A wait in vain takes about a second.
 constexpr uint32_t kPolls = 1u << 18;
 
@@ -40,13 +45,18 @@ constexpr uint32_t kPolls = 1u << 18;
 // warp's convergence: with a loop of its own for each lane, a vote behind it and arrivals by lane 0, lanes left one by one, and in some
 // builds lane 0 went on alone and the others waited for a phase that was over.  (One lane that polls for all: 202 us for 142 with 64 single
 // tokens over e4m3 caches.)
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  for (uint32_t i = 0; i < kPolls; ++i) {
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls) {
+  for (uint32_t i = 0; i < polls; ++i) {
     if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar, parity))) return true;
     if ((i & 255u) == 255u && __any_sync(0xffffffffu, *abort_flag)) return false;
   }
   *abort_flag = 1;
   return false;
+}
+// One thread waits for what is under way, whatever has given up.
+__device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
+  volatile int none = 0;
+  tc::mbar_wait_limited(bar, parity, &none, kPolls);
 }
 
 // One request as the kernels see it.  Offsets, lengths and positions that make no sense give it no rows or no keys.
@@ -216,20 +226,51 @@ template <> __device__ __forceinline__ uint32_t pack2of<__half>(float a, float b
   return *reinterpret_cast<const uint32_t*>(&t);
 }
 
+// NaN in the rows, and their log-sums, of the items that begin in the block's share.
+template <typename T, int ROWS, int KEYS, int OPEN, int DIM>
+__device__ __noinline__ void give_up_share(const Params& p) {
+  __shared__ long long scratch[128 / 32 + 4];
+  Cursor<ROWS, KEYS> at;
+  long long first, per;
+  const int count = find_share<ROWS, KEYS, 128, OPEN>(p, at, first, per, scratch);
+  const int row = blockIdx.y * 4 + warp_index(), lane = threadIdx.x & 31;
+  const float nan = __int_as_float(0x7fffffff);
+  for (int u = 0; u < count; ++u) {
+    const int r = at.tile * ROWS + row;
+    if (at.unit == 0 && r < at.r.rows) {
+      const long long token = token_of(p, at.r.q0, r);
+      const int qh = head_of(p, at.h, r);
+      uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM);
+      for (int e = lane; e < DIM / 2; e += 32) out[e] = pack2of<T>(nan, nan);
+      if (p.lse && lane == 0) p.lse[token * p.q_heads + qh] = nan;
+    }
+    if (u + 1 < count) at.next(p);
+  }
+}
+
 // Joins the shares of the items that no share holds alone: one warp per (item, row).  A share leaves at most one item open, its
 // last, which its own slot 1 and slot 0 of the following shares hold.
-template <typename T, int ROWS, int DIM>
-__global__ void __launch_bounds__(128) attend_join_kernel(Params p) {
+template <typename T, int ROWS, int KEYS, int OPEN, int DIM>
+__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ Params p) {
   wait_for_previous_kernel();
   const int share = blockIdx.x;
   const int4 item = p.open[2 * share], more = p.open[2 * share + 1];
   const int row = blockIdx.y * 4 + warp_index(), lane = threadIdx.x & 31;
+  if (more.y) {
+    give_up_share<T, ROWS, KEYS, OPEN, DIM>(p);
+    return;
+  }
   if (more.x <= share || row >= item.w) return;
   constexpr long long kSlot = (long long)ROWS * (DIM + 2);
   auto slot_of = [&](int s) { return p.part + (2ll * s + (s == share)) * kSlot; };
   float top = -INFINITY;
-  for (int s = share + lane; s <= more.x; s += 32) top = fmaxf(top, slot_of(s)[ROWS * DIM + row]);
+  int lost = 0;
+  for (int s = share + lane; s <= more.x; s += 32) {
+    top = fmaxf(top, slot_of(s)[ROWS * DIM + row]);
+    lost |= p.open[2 * s + 1].y;
+  }
   top = warp_max(top);
+  lost = __any_sync(0xffffffffu, lost != 0);
   const float safe = top == -INFINITY ? 0.f : top;
   constexpr int kPer = DIM / 32;
   float o[kPer], sum = 0.f;
@@ -252,6 +293,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(Params p) {
       o[0] += w * v.x; o[1] += w * v.y;
     }
   }
+  if (lost) sum = __int_as_float(0x7fffffff);
   const float inv = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
   const long long token = token_of(p, item.x, item.z + row);
   const int qh = head_of(p, item.y, item.z + row);

@@ -187,10 +187,12 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
       page = box < boxes && key < at.k.hi && key + rows > at.k.lo ? p.t.table[at.b * p.t.table_ld + (key >> p.c.page_shift)] : -1;
       if ((unsigned)page >= (unsigned)p.c.pages) page = -1;
     };
-    bool fresh = true, whole_start = false, ok = true;
+    bool fresh = true, whole_start = false, loose = false;      // loose: copies under way that no unit has been handed over with
     uint32_t phase = 1, part_phase = 0;
+    int filled = 0;                                            // units handed over
     look_up();
     for (int u = 0; u < count; ++u) {
+      if (share == p.stop_share && u == p.stop_unit) break;
       if (fresh) whole_start = at.unit == 0;
       const int key0 = at.key, row0 = at.tile * ROWS;
       const bool ends = at.unit + 1 == at.units;
@@ -213,7 +215,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         at.next(p);
         look_up();
       }
-      if (!(ok = warp_wait(empty + stage, phase, abort_flag))) break;
+      if (!warp_wait(empty + stage, phase, abort_flag, p.polls)) break;
       char* base = smem + stage * L::kStage;
       float* sc = reinterpret_cast<float*>(smem + kS * L::kStage) + stage * 2 * kKeys;
       uint64_t* bar = all == 0xffffffffu ? full + stage : partly;
@@ -237,7 +239,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                     rows * 4, bar);
       }
       if (all != 0xffffffffu) {                                // values of keys that are not there: zeros, whatever memory holds
-        if (!(ok = warp_wait(partly, part_phase, abort_flag))) break;
+        if ((loose = !warp_wait(partly, part_phase, abort_flag, p.polls))) break;
         part_phase ^= 1u;
 #pragma unroll
         for (int i = 0; i < kKeys / 32; ++i)
@@ -249,14 +251,15 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         fence_async_proxy();                                   // before copies into the same place
         mbar_arrive(full + stage);
       }
+      ++filled;
       if (++stage == kS) { stage = 0; phase ^= 1u; }
     }
-    // copies under way end before their memory goes, also after a wait that gave up
-    for (int i = 0; i < kS && !ok; ++i) {
-      volatile int gave_up = 0;
-      mbar_wait_limited(full + i, 0, &gave_up, 1u << 16);
-      mbar_wait_limited(full + i, 1, &gave_up, 1u << 16);
+    // copies under way end before their memory goes, whether or not the others are still there to wait for them
+    if (lane == 0) {
+      if (loose) drain(partly, part_phase);
+      for (int i = 0; i < min(filled, kS); ++i) drain(full + i, i < stage ? phase ^ 1u : phase);
     }
+    __syncwarp();
   } else {
     // ---------------- the computing warps ----------------
     const int wm = warp / kWarpsK, wk = warp % kWarpsK;
@@ -268,21 +271,19 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     int low = 0, high = 0;        // the lowest of them, the highest before the highest one's window
     int stage = 0;
     uint32_t phase = 0, met_phase = 0;
-    bool ok = true, inside = false;   // between an item's first unit and its last
     int q0 = 0, h = 0, tile_row = 0;  // the item at hand
     auto meet = [&] {
       mbar_arrive(met);
-      ok = warp_wait(met, met_phase, abort_flag) && ok;
+      warp_wait(met, met_phase, abort_flag, p.polls);
       met_phase ^= 1u;
     };
     for (int u = 0; u < count; ++u) {
-      if (!(ok = warp_wait(full + stage, phase, abort_flag) && ok)) break;
+      if (!warp_wait(full + stage, phase, abort_flag, p.polls)) break;
       const int4* say = reinterpret_cast<const int4*>(says + stage * L::kSay);
       const uint32_t* there = reinterpret_cast<const uint32_t*>(say + 2);
       const int flags = say[0].y;
       if (flags & kBegins) {
         const int4 a = say[0], b = say[1];
-        inside = true;
         q0 = a.z;
         h = a.w;
         tile_row = b.x;
@@ -494,7 +495,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             const int in = wm * 16 + g + 8 * i, r = tile_row + in;
             if (r < b.y) {
               if (whole) {
-                const float inv = !ok ? __int_as_float(0x7fffffff) : sum[i] > 0.f ? 1.f / sum[i] : (sum[i] == sum[i] ? 0.f : sum[i]);
+                const float inv = sum[i] > 0.f ? 1.f / sum[i] : (sum[i] == sum[i] ? 0.f : sum[i]);
                 const long long token = token_of(p, q0, r);
                 const int qh = head_of(p, h, r);
                 T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM;
@@ -509,7 +510,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                     *reinterpret_cast<uint32_t*>(out + j * 8 + 2 * tq) = pack2of<T>(o[j][2 * i] * inv, o[j][2 * i + 1] * inv);
                 }
                 if (p.lse && tq == 0)
-                  p.lse[token * p.q_heads + qh] = ok ? 0.69314718055994531f * ((top[i] == -INFINITY ? 0.f : top[i]) + log2f(sum[i])) : inv;
+                  p.lse[token * p.q_heads + qh] = 0.69314718055994531f * ((top[i] == -INFINITY ? 0.f : top[i]) + log2f(sum[i]));
               } else {
                 float* slot = p.part + (2 * share + ((flags & kWholeStart) != 0)) * (long long)(ROWS * (DIM + 2));
                 float* x = slot + in * DIM;
@@ -523,7 +524,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                 }
                 if (tq == 0) {
                   slot[ROWS * DIM + in] = top[i];
-                  slot[ROWS * (DIM + 1) + in] = ok ? sum[i] : __int_as_float(0x7fffffff);
+                  slot[ROWS * (DIM + 1) + in] = sum[i];
                 }
               }
             }
@@ -532,24 +533,14 @@ attend_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         if (u + 1 == count && tid == 0) {
           const bool open = !last && (flags & kWholeStart);
           p.open[2 * share] = make_int4(q0, h, tile_row, min(ROWS, b.y - tile_row));
-          p.open[2 * share + 1] = make_int4(open ? (int)((first + per + b.w - 1) / per) : -1, 0, 0, 0);
+          p.open[2 * share + 1].x = open ? (int)((first + per + b.w - 1) / per) : -1;
         }
-        inside = false;
       }
       mbar_arrive(empty + stage);
       if (++stage == kS) { stage = 0; phase ^= 1u; }
     }
-    if (!ok && inside && wk == 0) {                            // a wait gave up: the item at hand becomes NaN
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = tile_row + wm * 16 + g + 8 * i;
-        if (pos[i] < 0) continue;
-        T* out = static_cast<T*>(p.out) + token_of(p, q0, r) * p.out_ld + (long long)head_of(p, h, r) * DIM;
-        const uint32_t nan = pack2of<T>(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
-        for (int j = tq; j < DIM / 2; j += 4) reinterpret_cast<uint32_t*>(out)[j] = nan;
-      }
-    }
   }
+  if (lane == 0 && *abort_flag) p.open[2 * share + 1].y = 1;
   launch_dependents_now();
 }
 

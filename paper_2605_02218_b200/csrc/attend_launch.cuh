@@ -43,13 +43,13 @@ cudaError_t launch_rows(const Params& prm, const covspec_cache* cache, int ctas,
     return cudaErrorInvalidValue;
   e = launch_dependent(kernel, dim3((unsigned)ctas), kThreads, L::kSmem, s, map_k, map_v, prm);
   if (e != cudaSuccess) return e;
-  return launch_dependent(attend_join_kernel<T, ROWS, DIM>, dim3((unsigned)ctas, ROWS / 4), 128, 0, s, prm);
+  return launch_dependent(attend_join_kernel<T, ROWS, L::kKeys, kOpen, DIM>, dim3((unsigned)ctas, ROWS / 4), 128, 0, s, prm);
 }
 
 template <typename T, int STORE, int DIM>
 cudaError_t launch_wide(const Params& prm, const covspec_cache* cache, int ctas, cudaStream_t s) {
   constexpr auto kernel = wide::attend_wide_kernel<T, STORE, DIM>;
-  constexpr int smem = wide::Layout<STORE, DIM>::kSmem, rows = kWideRows;
+  constexpr int smem = wide::Layout<STORE, DIM>::kSmem;
   cudaError_t e = allow_shared<kernel>(smem);
   if (e != cudaSuccess) return e;
   CUtensorMap map_k{}, map_v{};
@@ -57,7 +57,7 @@ cudaError_t launch_wide(const Params& prm, const covspec_cache* cache, int ctas,
     return cudaErrorInvalidValue;
   e = launch_dependent(kernel, dim3((unsigned)ctas), wide::kThreads, smem, s, map_k, map_v, prm);
   if (e != cudaSuccess) return e;
-  return launch_dependent(attend_join_kernel<T, rows, DIM>, dim3((unsigned)ctas, rows / 4), 128, 0, s, prm);
+  return launch_dependent(attend_join_kernel<T, kWideRows, kWideKeys, wide::kOpen, DIM>, dim3((unsigned)ctas, kWideRows / 4), 128, 0, s, prm);
 }
 
 template <typename T, int STORE, int DIM>

@@ -138,11 +138,6 @@ __device__ __forceinline__ int tile_at(int rows, int row, int chunk) {
   return (chunk >> 3) * rows * 128 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
 }
 
-template <typename T> __device__ __forceinline__ T pack_nan() {
-  const uint32_t w = pack2of<T>(__int_as_float(0x7fffffff), 0.f);
-  return *reinterpret_cast<const T*>(&w);
-}
-
 template <typename T, int STORE, int DIM>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p) {
@@ -176,8 +171,8 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   long long first, per;
   const int count = find_share<kRows, kKeys, kThreads, kOpen>(p, at, first, per, reinterpret_cast<long long*>(exchange));
   const int share = blockIdx.x;
+  if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
   if (count <= 0) {
-    if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
     launch_dependents_now();
     return;
   }
@@ -193,17 +188,18 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const int wp = warp - kSoftmaxWarps - 1;
     int slot = 0;
     uint32_t phase = 1, q_phase = 1;
-    bool ok = true, fresh = true;
-    auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
-    auto queries = [&] {                                       // of the item at `at`
-      ok = ok && warp_wait(q_empty, q_phase, abort_flag);
+    bool fresh = true, loose = false;                          // loose: copies under way in a slot that has not been handed over
+    int filled = 0;                                            // slots handed over
+    auto next_slot = [&] { ++filled; if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
+    auto queries = [&] {                                       // of the item at `at`; false: a wait gave up
+      if (!warp_wait(q_empty, q_phase, abort_flag, p.polls)) return false;
       q_phase ^= 1u;
       constexpr int kChunks = DIM / 8, kAtOnce = 32 / kChunks, kStep = kCopyWarps * kAtOnce;
       const int chunk = lane % kChunks;
       // token and query head of row r, and how far they go on from one of this thread's rows to the next
       int row = wp * kAtOnce + lane / kChunks;
       int token = (at.tile * kRows + row) / p.group, head = at.tile * kRows + row - token * p.group;
-      const int step_token = kStep / p.group, step_head = kStep - step_token * p.group, rows = ok ? at.r.rows - at.tile * kRows : 0;
+      const int step_token = kStep / p.group, step_head = kStep - step_token * p.group, rows = at.r.rows - at.tile * kRows;
       const T* q0 = static_cast<const T*>(p.q) + at.r.q0 * p.q_ld + (long long)at.h * p.group * DIM + chunk * 8;
 #pragma unroll 4
       for (int i = 0; i < (kRows + kStep - 1) / kStep; ++i, row += kStep) {
@@ -219,11 +215,12 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       copies_wait<0>();
       fence_async_proxy();
       mbar_arrive(q_full);
+      return true;
     };
     {
       if (wp > 0) {                                            // these two only help with the queries
-        for (int u = 0; u < count && ok; ++u) {
-          if (fresh) queries();
+        for (int u = 0; u < count; ++u) {
+          if (fresh && !queries()) break;
           fresh = at.unit + 1 == at.units;
           if (u + 1 < count) at.next(p);
         }
@@ -239,10 +236,11 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         bool whole_start = false;
         uint32_t part_phase = 0;
         look_up_box();
-        for (int u = 0; u < count && ok; ++u) {
+        for (int u = 0; u < count; ++u) {
+          if (share == p.stop_share && u == p.stop_unit) break;
           const bool begins = fresh;
           if (begins) {
-            queries();
+            if (!queries()) break;
             whole_start = at.unit == 0;
           }
           const int row0 = at.tile * kRows, key0 = at.key, page_row = (at.h << p.c.page_shift) + ((key0 + (box << shift)) & mask);
@@ -264,7 +262,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             look_up_box();
           }
           // the words of unit u - 4 have been read: its products are done (the slot that this unit's keys take says so)
-          if (!(ok = warp_wait(empty + slot, phase, abort_flag))) break;
+          if (!warp_wait(empty + slot, phase, abort_flag, p.polls)) break;
           if (lane == 0) {
             *reinterpret_cast<uint4*>(there + (u & 3) * 4) = make_uint4(word[0], word[1], word[2], word[3]);
             units[(u & 3) * 2] = item[0];
@@ -276,7 +274,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           __syncwarp();
           if (mine) tma_load_3d(smem_u32(ring + slot * L::kSlot) + part * (kKeys * 128) + (box << shift) * 128, &map_k, part * 64, page_row, box_page, full + slot);
           next_slot();
-          if (!(ok = warp_wait(empty + slot, phase, abort_flag))) break;
+          if (!warp_wait(empty + slot, phase, abort_flag, p.polls)) break;
           const bool all = (word[0] & word[1] & word[2] & word[3]) == 0xffffffffu;
           uint64_t* bar = all ? full + slot : partly;
           if (lane == 0) mbar_expect_tx(bar, bytes);
@@ -284,9 +282,8 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           __syncwarp();
           if (mine) tma_load_3d(smem_u32(ring + slot * L::kSlot) + part * (kKeys * 128) + (box << shift) * 128, &map_v, part * 64, page_row, box_page, bar);
           if (!all) {                                          // values of keys that are not there: zeros, whatever memory holds
-            ok = warp_wait(partly, part_phase, abort_flag);
+            if ((loose = !warp_wait(partly, part_phase, abort_flag, p.polls))) break;
             part_phase ^= 1u;
-            if (!ok) break;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (!((word[i] >> lane) & 1u))
@@ -297,12 +294,12 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           }
           next_slot();
         }
-        // copies under way end before their memory goes: the slots' barriers say so, also after a wait that gave up
-        for (int i = 0; i < kSlots && !ok; ++i) {
-          volatile int gave_up = 0;
-          mbar_wait_limited(full + i, 0, &gave_up, 1u << 16);
-          mbar_wait_limited(full + i, 1, &gave_up, 1u << 16);
+        // copies under way end before their memory goes, whether or not the others are still there to wait for them
+        if (lane == 0) {
+          if (loose) drain(partly, part_phase);
+          for (int i = 0; i < min(filled, kSlots); ++i) drain(full + i, i < slot ? phase ^ 1u : phase);
         }
+        __syncwarp();
       }
     }
   } else if (warp == kSoftmaxWarps) {
@@ -313,7 +310,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       uint32_t phase = 0, q_phase = 0, p_phase = 0;
       bool ok = true;
       auto next_slot = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
-      auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = ok && mbar_wait_limited(bar, parity, abort_flag, kPolls); };
+      auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = ok && mbar_wait_limited(bar, parity, abort_flag, p.polls); };
       auto scores = [&](int x, int s) {
         const uint32_t a0 = smem_u32(smem + x * (128 * DIM * 2)), b0 = smem_u32(ring + s * L::kSlot);
 #pragma unroll
@@ -371,8 +368,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
       // TMEM and the ring are free when every product has ended, also after a wait that gave up
       umma_commit(drained);
-      volatile int gave_up = 0;
-      mbar_wait_limited(drained, 0, &gave_up, kPolls);
+      drain(drained, 0);
     }
     __syncwarp();
   } else {
@@ -384,20 +380,11 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     float* shared = exchange + x * 128 + row;
     float ref = 0.f, sum = 0.f;
     int pos = -1;                                              // position of the row's token
-    bool ok = true, active = false;
+    bool active = false;
     uint32_t s_phase = 0, o_phase = 0;
-    if (tid == 0) p.open[2 * share + 1] = make_int4(-1, 0, 0, 0);
     for (int u = 0; u < count; ++u) {
       // the two warps of a row go on or give up together: they meet at barriers further down
-      ok = barrier_and(pair, 64, warp_wait(s_full + x, s_phase, abort_flag));
-      if (!ok) {                                               // it gave up: the item at hand becomes NaN
-        const int4 first_half = units[((u - 1) & 3) * 2], item = units[((u - 1) & 3) * 2 + 1];
-        const int r = item.x + x * 128 + row;
-        if (u > 0 && !(first_half.y & kEnds) && r < item.y)
-          for (int e = half * (DIM / 2); e < (half + 1) * (DIM / 2); ++e)
-            static_cast<T*>(p.out)[token_of(p, first_half.z, r) * p.out_ld + (long long)head_of(p, first_half.w, r) * DIM + e] = pack_nan<T>();
-        break;
-      }
+      if (!barrier_and(pair, 64, warp_wait(s_full + x, s_phase, abort_flag, p.polls))) break;
       s_phase ^= 1u;
       tc_fence_after();
       __syncwarp();
@@ -509,7 +496,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const bool whole = (flags & kEnds) && (flags & kWholeStart);
         const int q0 = units[(u & 3) * 2].z, h = units[(u & 3) * 2].w;
         if (active) {
-          ok = warp_wait(o_full + x, o_phase, abort_flag);
+          warp_wait(o_full + x, o_phase, abort_flag, p.polls); // both warps of a row go on, whatever it says
           o_phase ^= 1u;
           tc_fence_after();
           const int r = item.x + x * 128 + row;
@@ -520,8 +507,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           if (!half) *shared = total = sum + *shared;
           meet_at(pair, 64);
           if (half) total = *shared;
-          // a wait that gave up leaves NaN
-          const float inv = !ok ? __int_as_float(0x7fffffff) : total > 0.f ? 1.f / total : (total == total ? 0.f : total);
+          const float inv = total > 0.f ? 1.f / total : (total == total ? 0.f : total);
           const long long token = is ? token_of(p, q0, r) : 0;
           const int qh = is ? head_of(p, h, r) : 0;
           T* out = static_cast<T*>(p.out) + token * p.out_ld + (long long)qh * DIM + half * (DIM / 2);
@@ -545,9 +531,9 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           if (is && half == 0) {
             if (!whole) {
               slot[kRows * DIM + in] = ref;
-              slot[kRows * (DIM + 1) + in] = ok ? total : inv;
+              slot[kRows * (DIM + 1) + in] = total;
             } else if (p.lse) {
-              p.lse[token * p.q_heads + qh] = ok ? 0.69314718055994531f * ((ref == -INFINITY ? 0.f : ref) + log2f(total)) : inv;
+              p.lse[token * p.q_heads + qh] = 0.69314718055994531f * ((ref == -INFINITY ? 0.f : ref) + log2f(total));
             }
           }
           tc_fence_before();
@@ -555,7 +541,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         if (u + 1 == count && tid == 0) {
           const bool open = !(flags & kEnds) && (flags & kWholeStart);
           p.open[2 * share] = make_int4(q0, h, item.x, min(kRows, item.y - item.x));
-          p.open[2 * share + 1] = make_int4(open ? (int)((first + per + item.w - 1) / per) : -1, 0, 0, 0);
+          p.open[2 * share + 1].x = open ? (int)((first + per + item.w - 1) / per) : -1;
         }
       }
     }
@@ -564,6 +550,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   __syncthreads();
   tc_fence_after();
   if (warp == kSoftmaxWarps) tmem_dealloc(tmem, 512);
+  if (tid == 0 && *abort_flag) p.open[2 * share + 1].y = 1;
   launch_dependents_now();
 }
 

@@ -85,6 +85,62 @@ int cache_grid(int rows, int lanes, int passes) {
 
 long long part_bytes(int ctas, int rows, int dim) { return 2ll * ctas * rows * (dim + 2) * 4; }
 
+int cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q, long long q_stride,
+                 int q_heads, float scale, int window, int max_new, void* out, long long out_stride, float* lse, void* workspace,
+                 long long workspace_bytes, uint32_t polls, int stop_share, int stop_unit, void* stream) {
+  int st = check_cache(cache);
+  if (st == COVSPEC_OK) st = check_tokens(tokens);
+  if (st != COVSPEC_OK) return st;
+  if (dtype != COVSPEC_BF16 && dtype != COVSPEC_F16) return COVSPEC_ERR_UNSUPPORTED;
+  if (cache->store != dtype && cache->store < COVSPEC_E4M3) return COVSPEC_ERR_UNSUPPORTED;
+  if (n < 0 || q_heads < 1 || q_heads % cache->heads || (long long)n * q_heads > INT_MAX / 2) return COVSPEC_ERR_SHAPE;
+  if (window < 0 || max_new < 0 || !(scale == scale)) return COVSPEC_ERR_ARG;
+  if (n == 0) return COVSPEC_OK;
+  const long long width = (long long)q_heads * cache->head_dim;
+  if (!q || !out || !workspace || !aligned16(q) || !aligned16(out) || !aligned16(workspace)) return COVSPEC_ERR_ARG;
+  if (q_stride < width || out_stride < width) return COVSPEC_ERR_SHAPE;
+  if (q_stride % 8 || out_stride % 8) return COVSPEC_ERR_ARG;
+  const long long need = covspec_cache_attend_workspace(cache, q_heads);
+  if (need < 0) return (int)need;
+  if (workspace_bytes < need) return COVSPEC_ERR_WORKSPACE;
+  int sms = 0;
+  if (const int e = sm_count(&sms)) return e;
+
+  attend::Params prm{};
+  prm.c = pages_of(cache);
+  prm.t = tokens_of(tokens);
+  prm.q = q; prm.out = out; prm.lse = lse;
+  prm.q_ld = q_stride; prm.out_ld = out_stride;
+  prm.n = n; prm.q_heads = q_heads; prm.group = q_heads / cache->heads;
+  prm.window = std::min(window, 1 << 30);
+  prm.scale_log2 = scale * 1.4426950408889634f;
+  prm.rows_over = 0; prm.rows_upto = INT_MAX;
+  prm.least_units = 1;
+  prm.polls = polls; prm.stop_share = stop_share; prm.stop_unit = stop_unit;
+  prm.open = static_cast<int4*>(workspace);
+  prm.part = reinterpret_cast<float*>(prm.open + 2ll * (attend::kRowsCtas + 1) * sms);
+  // rows of a key head in the largest request.  Where some may have many, each of the two kernels takes its requests
+  const long long most = (long long)(max_new > 0 ? std::min(max_new, n) : n) * prm.group;
+  const int rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+  const bool both = most > attend::kFewRows && cache->store < COVSPEC_E4M3;
+  // no more CTAs than there can be units
+  auto ctas_of = [&](int rows, int keys, int ctas) {
+    const long long items = ((long long)n * prm.group / rows + prm.t.batch) * cache->heads;
+    return (int)std::min<long long>(ctas, items * (((long long)prm.t.width * cache->page_size + keys - 1) / keys + 1));
+  };
+  const int ctas = ctas_of(rows, 64, attend::kRowsCtas * sms);
+  attend::Params wide = prm;
+  wide.rows_over = attend::kFewRows;
+  wide.open = prm.open + 2ll * attend::kRowsCtas * sms;
+  wide.part = prm.part + part_bytes(attend::kRowsCtas * sms, attend::kFewRows, cache->head_dim) / 4;
+  const int wide_ctas = ctas_of(attend::kWideRows, attend::kWideKeys, sms);
+  if (both) prm.rows_upto = attend::kFewRows;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const attend::Call call{prm, wide, cache, rows, ctas, both ? wide_ctas : 0, s};
+  CUDA_TRY(dtype == COVSPEC_BF16 ? attend::launch_bf16(call) : attend::launch_f16(call));
+  return COVSPEC_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -158,56 +214,16 @@ long long covspec_cache_attend_workspace(const covspec_cache* cache, int q_heads
 int covspec_cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
                          long long q_stride, int q_heads, float scale, int window, int max_new, void* out, long long out_stride,
                          float* lse, void* workspace, long long workspace_bytes, void* stream) {
-  int st = check_cache(cache);
-  if (st == COVSPEC_OK) st = check_tokens(tokens);
-  if (st != COVSPEC_OK) return st;
-  if (dtype != COVSPEC_BF16 && dtype != COVSPEC_F16) return COVSPEC_ERR_UNSUPPORTED;
-  if (cache->store != dtype && cache->store < COVSPEC_E4M3) return COVSPEC_ERR_UNSUPPORTED;
-  if (n < 0 || q_heads < 1 || q_heads % cache->heads || (long long)n * q_heads > INT_MAX / 2) return COVSPEC_ERR_SHAPE;
-  if (window < 0 || max_new < 0 || !(scale == scale)) return COVSPEC_ERR_ARG;
-  if (n == 0) return COVSPEC_OK;
-  const long long width = (long long)q_heads * cache->head_dim;
-  if (!q || !out || !workspace || !aligned16(q) || !aligned16(out) || !aligned16(workspace)) return COVSPEC_ERR_ARG;
-  if (q_stride < width || out_stride < width) return COVSPEC_ERR_SHAPE;
-  if (q_stride % 8 || out_stride % 8) return COVSPEC_ERR_ARG;
-  const long long need = covspec_cache_attend_workspace(cache, q_heads);
-  if (need < 0) return (int)need;
-  if (workspace_bytes < need) return COVSPEC_ERR_WORKSPACE;
-  int sms = 0;
-  if (const int e = sm_count(&sms)) return e;
+  return cache_attend(cache, tokens, dtype, n, q, q_stride, q_heads, scale, window, max_new, out, out_stride, lse, workspace,
+                      workspace_bytes, attend::kPolls, -1, 0, stream);
+}
 
-  attend::Params prm{};
-  prm.c = pages_of(cache);
-  prm.t = tokens_of(tokens);
-  prm.q = q; prm.out = out; prm.lse = lse;
-  prm.q_ld = q_stride; prm.out_ld = out_stride;
-  prm.n = n; prm.q_heads = q_heads; prm.group = q_heads / cache->heads;
-  prm.window = std::min(window, 1 << 30);
-  prm.scale_log2 = scale * 1.4426950408889634f;
-  prm.rows_over = 0; prm.rows_upto = INT_MAX;
-  prm.least_units = 1;
-  prm.open = static_cast<int4*>(workspace);
-  prm.part = reinterpret_cast<float*>(prm.open + 2ll * (attend::kRowsCtas + 1) * sms);
-  // rows of a key head in the largest request.  Where some may have many, each of the two kernels takes its requests
-  const long long most = (long long)(max_new > 0 ? std::min(max_new, n) : n) * prm.group;
-  const int rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
-  const bool both = most > attend::kFewRows && cache->store < COVSPEC_E4M3;
-  // no more CTAs than there can be units
-  auto ctas_of = [&](int rows, int keys, int ctas) {
-    const long long items = ((long long)n * prm.group / rows + prm.t.batch) * cache->heads;
-    return (int)std::min<long long>(ctas, items * (((long long)prm.t.width * cache->page_size + keys - 1) / keys + 1));
-  };
-  const int ctas = ctas_of(rows, 64, attend::kRowsCtas * sms);
-  attend::Params wide = prm;
-  wide.rows_over = attend::kFewRows;
-  wide.open = prm.open + 2ll * attend::kRowsCtas * sms;
-  wide.part = prm.part + part_bytes(attend::kRowsCtas * sms, attend::kFewRows, cache->head_dim) / 4;
-  const int wide_ctas = ctas_of(attend::kWideRows, attend::kWideKeys, sms);
-  if (both) prm.rows_upto = attend::kFewRows;
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const attend::Call call{prm, wide, cache, rows, ctas, both ? wide_ctas : 0, s};
-  CUDA_TRY(dtype == COVSPEC_BF16 ? attend::launch_bf16(call) : attend::launch_f16(call));
-  return COVSPEC_OK;
+int covspec_selftest_attend_timeout(const covspec_cache* cache, const covspec_tokens* tokens, int dtype, int n, const void* q,
+                                    long long q_stride, int q_heads, float scale, int window, int max_new, void* out,
+                                    long long out_stride, float* lse, void* workspace, long long workspace_bytes, int block, int unit,
+                                    void* stream) {
+  return cache_attend(cache, tokens, dtype, n, q, q_stride, q_heads, scale, window, max_new, out, out_stride, lse, workspace,
+                      workspace_bytes, block < 0 ? 0u : attend::kPolls / 16, std::max(block, -1), unit, stream);
 }
 
 int covspec_edit_logits(int logit_dtype, int rows, int vocab, long long ld, const void* z, void* out, const covspec_edits* edits,

@@ -1,11 +1,13 @@
-"""The attention over the paged cache where value scales are of very different size and where offsets reach past the call's rows.
-All rows are held against the definition in 64 bits, on the GPU."""
+"""The attention over the paged cache where value scales are of very different size and where offsets reach past the call's rows: all
+rows against the definition in 64 bits, on the GPU.  And what it leaves where a wait inside its kernels gives up."""
+import ctypes as C
 import math
 
 import numpy as np
 import pytest
 import torch
 
+from paper_2605_02218_b200 import api
 from tests.test_gpu_verify import DEV, TYPES, Paged, half, i32, prefix
 
 pytestmark = pytest.mark.gpu
@@ -131,6 +133,103 @@ def test_offsets_that_make_no_sense_give_no_keys(window):
     assert (out[3:] == 0).all() and (lse[3:] == -math.inf).all()
     p.new = [3]
     check(p, q[:3], out[:3], lse[:3], 0.125, window if window < 2 ** 31 - 1 else 0)
+
+
+# ---- waits that give up -------------------------------------------------------------------------------------------------
+
+def shares(p, group, window, rows, keys, opening, ctas, over=0, upto=2 ** 31 - 1):
+    """For each block, (request, head, tile) of every unit of its share: the line of items and units, cut into equal shares."""
+    line = []
+    for b, (m, length) in enumerate(zip(p.new, p.length)):
+        n = m * group
+        if not over < n <= upto:
+            continue
+        items = []
+        for tile in range(-(-n // rows)):
+            first, last = tile * rows, min((tile + 1) * rows, n) - 1
+            hi = max(min(length - m + last // group + 1, length), 0)
+            lo = max(length - m + first // group - window + 1, 0) if window else 0
+            items.append((hi - 1) // keys - lo // keys + 1 if hi > lo else 1)
+        line += [x for h in range(p.heads) for t, u in enumerate(items) for x in [None] * opening + [(b, h, t)] * u]
+    per = max(-(-len(line) // ctas), 1)
+    return [[x for x in line[i * per:(i + 1) * per] if x is not None] for i in range(ctas)]
+
+
+def kernels_of(p, dtype, q_heads, window, most):
+    """Shares of the kernel for few rows and, where it runs, of the one for many; rows of their items."""
+    sms, group, n = torch.cuda.get_device_properties(0).multi_processor_count, q_heads // p.heads, sum(p.new)
+    top = (min(most, n) if most else n) * group
+    rows = 16 if top <= 16 else 32 if top <= 32 else 64
+    held = p.store in ("e4m3", "int8")
+    both = top > 64 and not held
+
+    def ctas(rows, keys, most):
+        return min(most, (n * group // rows + len(p.new)) * p.heads * (-(-p.table.shape[1] * p.page // keys) + 1))
+    few = shares(p, group, window, rows, 128 if held and rows < 64 else 64, 2, ctas(rows, 64, 2 * sms), 0, 64 if both else 2 ** 31 - 1)
+    got = [(few, rows)]
+    if both:
+        got.append((shares(p, group, window, 256, 128, 4, ctas(256, 128, sms), 64), 256))
+    return got
+
+
+def selftest(p, q, window, most, block, unit):
+    """The call with waits that give up; its scratch holds plausible numbers before."""
+    n, heads = q.shape[:2]
+    out = torch.full_like(q, 3.0)
+    lse = torch.full((n, heads), 3.0, device=DEV)
+    lib = api.load_library()
+    size = lib.covspec_cache_attend_workspace(p.cache._ref, heads)
+    work = torch.ones(size // 4, device=DEV)
+    st = lib.covspec_selftest_attend_timeout(p.cache._ref, C.byref(p.cache._tokens(*p.tokens())), api._LOGIT_DTYPES[q.dtype], n, q.data_ptr(),
+                                             heads * p.dim, heads, p.dim ** -0.5, window, most, out.data_ptr(), heads * p.dim,
+                                             lse.data_ptr(), work.data_ptr(), size, block, unit, api._raw_stream())
+    assert st == 0
+    torch.cuda.synchronize()
+    return out, lse
+
+
+GIVEN_UP = [("bf16", "bf16", 128, [1, 4, 0, 2], [3000, 900, 70, 2000], 2, 0, 4),
+            ("bf16", "bf16", 64, [1, 4, 0, 2] * 10, [3000, 1900, 70, 5000] * 10, 2, 0, 4),
+            ("bf16", "e4m3", 128, [1, 4, 2] * 16, [3000, 900, 6000] * 16, 2, 0, 4), ("f16", "int8", 64, [40, 130] * 5, [800, 1900] * 5, 3, 0, 0),
+            ("bf16", "bf16", 128, [300, 1, 700] * 4, [2500, 900, 3800] * 4, 4, 0, 0), ("f16", "f16", 64, [90, 400], [2500, 1000], 3, 500, 0)]
+
+
+@pytest.mark.parametrize("dtype,store,dim,new,length,group,window,most", GIVEN_UP)
+def test_rows_are_nan_where_every_wait_gives_up(dtype, store, dim, new, length, group, window, most):
+    p = Paged(85, store, 2, dim, 16, new, length)
+    q = torch.randn(sum(new) + 2, 2 * group, dim, device=DEV).to(TYPES[dtype])
+    want = p.cache.attend(q, *p.tokens(), window=window, max_new=most, lse=True)
+    out, lse = selftest(p, q, window, most, -1, 0)
+    n = sum(new)
+    assert out[:n].isnan().all() and lse[:n].isnan().all() and (out[n:] == 3).all() and (lse[n:] == 3).all()
+    again = p.cache.attend(q, *p.tokens(), window=window, max_new=most, lse=True)
+    assert all(torch.equal(a[:n], b[:n]) for a, b in zip(want, again))
+
+
+@pytest.mark.parametrize("dtype,store,dim,new,length,group,window,most", GIVEN_UP)
+def test_the_rows_that_a_block_had_a_part_of_are_nan_where_its_waits_give_up(dtype, store, dim, new, length, group, window, most):
+    p = Paged(86, store, 2, dim, 16, new, length)
+    heads, n = 2 * group, sum(new)
+    q = torch.randn(n, heads, dim, device=DEV).to(TYPES[dtype])
+    want = p.cache.attend(q, *p.tokens(), window=window, max_new=most, lse=True)
+    kernels = kernels_of(p, dtype, heads, window, most)
+    at = np.concatenate([[0], np.cumsum(new)])
+    used = sorted({i for ks, _ in kernels for i, s in enumerate(ks) if s})
+    cut = 0
+    for block in sorted({0} | {used[len(used) * i // 5] for i in range(5)} | {used[-1]}):
+        for unit in (0, 1, 3, 9):
+            lost = torch.zeros(n, heads, dtype=torch.bool, device=DEV)
+            for ks, rows in kernels:
+                if block >= len(ks) or unit >= len(ks[block]):
+                    continue
+                cut += any(len({i for i, s in enumerate(ks) if item in s}) > 1 for item in set(ks[block]))
+                for b, h, tile in set(ks[block]):
+                    r = torch.arange(tile * rows, min((tile + 1) * rows, new[b] * group), device=DEV)
+                    lost[at[b] + r // group, h * group + r % group] = True
+            out, lse = selftest(p, q, window, most, block, unit)
+            assert torch.equal(out.isnan().all(-1), lost) and torch.equal(lse.isnan(), lost), (block, unit)
+            assert torch.equal(out[~lost], want[0][~lost]) and torch.equal(lse[~lost], want[1][~lost])
+    assert cut                                                   # items that several blocks share were among them
 
 
 # ---- no wait in vain ----------------------------------------------------------------------------------------------------
