@@ -6,6 +6,8 @@
 #include <atomic>
 #include <string>
 
+#include "covspec.h"
+
 namespace covspec {
 
 inline thread_local std::string g_cuda_error;
@@ -18,6 +20,20 @@ inline thread_local std::string g_cuda_error;
       return COVSPEC_ERR_CUDA;                                                          \
     }                                                                                   \
   } while (0)
+
+// A step that may have said itself, in g_cuda_error, what failed; else the text is made of its status.
+template <typename F>
+int status_of(const char* what, F step) {
+  std::string before;
+  before.swap(g_cuda_error);
+  const cudaError_t e = step();
+  if (e == cudaSuccess) {
+    g_cuda_error.swap(before);
+    return COVSPEC_OK;
+  }
+  if (g_cuda_error.empty()) g_cuda_error = std::string(what) + ": " + cudaGetErrorString(e);
+  return COVSPEC_ERR_CUDA;
+}
 
 // Launch that may overlap the end of the kernel before it on the stream; the kernel calls
 // wait_for_previous_kernel (common.cuh) before it uses anything of that kernel's.  About 2 us less between two

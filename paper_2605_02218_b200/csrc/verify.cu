@@ -137,8 +137,7 @@ int cache_attend(const covspec_cache* cache, const covspec_tokens* tokens, int d
   if (both) prm.rows_upto = attend::kFewRows;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const attend::Call call{prm, wide, cache, rows, ctas, both ? wide_ctas : 0, s};
-  CUDA_TRY(dtype == COVSPEC_BF16 ? attend::launch_bf16(call) : attend::launch_f16(call));
-  return COVSPEC_OK;
+  return status_of("attention", [&] { return dtype == COVSPEC_BF16 ? attend::launch_bf16(call) : attend::launch_f16(call); });
 }
 
 }  // namespace
