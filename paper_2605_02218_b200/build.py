@@ -2,18 +2,21 @@
 is a plain C ABI loaded through ctypes), and the native part of the Python binding with g++ against torch's headers."""
 from __future__ import annotations
 
+import hashlib
 import os
 import re
 import subprocess
 import sys
 import sysconfig
+import time
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcovspec.so")
 LIB_DEBUG = os.path.join(HERE, "libcovspec_debug.so")     # the same sources with -DCOVSPEC_DEBUG_BOUNDS
-OBJECTS = os.path.join(HERE, "_build")                    # a compiled source is used again until one of its files changes
+OBJECTS = os.path.join(HERE, "_build")                    # a compiled source is used again until one of its files, its command or the
+                                                          # compiler changes
 SOURCES = ["covspec.cu", "verify.cu", "attend_bf16.cu", "attend_f16.cu"]
 BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
 
@@ -70,25 +73,29 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
               "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if debug_bounds:
         common.append("-DCOVSPEC_DEBUG_BOUNDS")
-    if verbose:
-        common += ["-Xptxas", "-v"]
     os.makedirs(OBJECTS, exist_ok=True)
+    # objects of another command or compiler are not linked with these
+    version = subprocess.run([nvcc, "--version"], capture_output=True, text=True).stdout
+    key = hashlib.sha256("\0".join([*common, version]).encode()).hexdigest()[:12]
     objects, running = [], []
     for name in SOURCES:
         source = os.path.join(CSRC, name)
-        objects.append(os.path.join(OBJECTS, os.path.splitext(name)[0] + ("_debug.o" if debug_bounds else ".o")))
-        if force or not os.path.exists(objects[-1]) or _newest(_files_of(source)) > os.path.getmtime(objects[-1]):
+        objects.append(os.path.join(OBJECTS, f"{os.path.splitext(name)[0]}{'_debug' if debug_bounds else ''}-{key}.o"))
+        # verbose: what the compiler says of every source
+        if force or verbose or not os.path.exists(objects[-1]) or _newest(_files_of(source)) > os.path.getmtime(objects[-1]):
             # under a name of its own until it is whole: what is there later is complete
             part = f"{objects[-1]}.{os.getpid()}.part"
-            running.append((objects[-1], part, subprocess.Popen([*common, "-o", part, source], stdout=subprocess.PIPE,
-                                                                stderr=subprocess.STDOUT, text=True)))
+            began = time.time()
+            running.append((objects[-1], part, began, subprocess.Popen([*common, *(["-Xptxas", "-v"] if verbose else []), "-o", part, source],
+                                                                       stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = False
-    for path, part, job in running:
+    for path, part, began, job in running:
         said = job.communicate()[0]
         failed |= job.returncode != 0
         if job.returncode or verbose:
             sys.stderr.write(said)
         if not job.returncode:
+            os.utime(part, (began, began))            # a file that changes while it is read is newer than what was made of it
             os.replace(part, path)
     if not failed:
         res = subprocess.run([nvcc, "-shared", "-Xcompiler", "-fPIC", *target, "-o", LIB, *objects], capture_output=True, text=True)
