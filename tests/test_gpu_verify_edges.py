@@ -1,5 +1,6 @@
-"""The attention over the paged cache where value scales are of very different size and where offsets reach past the call's rows: all
-rows against the definition in 64 bits, on the GPU.  And what it leaves where a wait inside its kernels gives up."""
+"""The paged cache and the attention over it where the first tests do not go: value scales of very different size, scores that grow
+along the keys, calls of several items a block, layouts of the caller's own, offsets past the call's rows, all rows against the
+definition in 64 bits on the GPU; the way from the pruning into the cache; and what is left where a wait inside the kernels gives up."""
 import ctypes as C
 import math
 
@@ -7,7 +8,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2605_02218_b200 import api
+from paper_2605_02218_b200 import api, workloads
 from tests.test_gpu_verify import DEV, TYPES, Paged, half, i32, prefix
 
 pytestmark = pytest.mark.gpu
@@ -78,14 +79,11 @@ def value_scale(p, b, first, last, by, keep):
         spot.copy_(spot * by if keep else torch.full_like(spot, by))
 
 
-@pytest.mark.parametrize("store,dtype", [("e4m3", "bf16"), ("int8", "bf16"), ("e4m3", "f16")])
+@pytest.mark.parametrize("store,dtype,high", [("e4m3", "f16", 1.0)] + [(s, "bf16", h) for s in ("e4m3", "int8") for h in (1.0, 2.0 ** 20, 2.0 ** 100)])
 @pytest.mark.parametrize("low", [0.0, 2.0 ** -149, 2.0 ** -126, 2.0 ** -100, 2.0 ** -60])
-@pytest.mark.parametrize("high", [1.0, 2.0 ** 20, 2.0 ** 100])
 @pytest.mark.parametrize("dim,group,new", [(64, 1, [1, 1, 1]), (128, 4, [3, 1, 70])])
 def test_rows_of_zeros_and_of_large_values_in_one_cache(store, dtype, low, high, dim, group, new):
     # whole units of keys with the least scales there are, before, after and without ordinary ones: they count in the sums
-    if dtype == "f16" and high != 1.0:
-        pytest.skip("the values are not numbers of the type")
     p = Paged(70, store, 1, dim, 16, new, [400, 70, 420])
     value_scale(p, 0, 0, 200, low, False)
     value_scale(p, 0, 200, 400, high, True)
@@ -111,6 +109,131 @@ def test_zero_rows_whose_keys_win_by_little(store):
     out, lse = p.cache.attend(q, prefix([2] * n), i32([300] * n), p.d_table.expand(n, -1).contiguous(), scale=1.0, lse=True)
     for i in range(0, 2 * n, 26):
         check(p, q[i:i + 2], out[i:i + 2], lse[i:i + 2], 1.0)
+
+
+# ---- scores that grow along the keys ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,store", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "int8")])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new,group,window", [([3, 8], 4, 0), ([150, 300], 3, 0), ([300, 150], 2, 400)])
+def test_references_that_move_from_unit_to_unit(dtype, store, dim, new, group, window):
+    # score of key t: about c * t / 100, with a slope c of each row's own, positive and negative: accumulated rows and sums are
+    # brought to new references by factors between 0 and 1, row by row at different keys
+    p = Paged(72, store, 2, dim, 16, new, [900, 700])
+    k = 0.3 * p.k
+    t = torch.cat([torch.arange(n, device=DEV) for n in p.length]).float()
+    k[:, :, 0] = t[:, None] / 100
+    p.cache.write(k, p.v, prefix(p.length), p.lengths, p.d_table)
+    n = sum(new)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    q = torch.randn(n, 2 * group, dim, generator=g, device=DEV)
+    q[:, :, 0] = torch.linspace(-6, 14, n * 2 * group, device=DEV).view(n, -1)[torch.randperm(n, generator=g, device=DEV)]
+    q = q.to(TYPES[dtype])
+    out, lse = p.cache.attend(q, *p.tokens(), scale=1.0, window=window, lse=True)
+    check(p, q, out, lse, 1.0, window)
+
+
+# ---- several items a block ----------------------------------------------------------------------------------------------
+
+def steps_a_share(p, group, window, rows=256, keys=128, opening=4):
+    """Places of the line of items and units that one block of the kernel for many rows takes, and the longest item's."""
+    total = longest = 0
+    for m, length in zip(p.new, p.length):
+        for tile in range(-(-m * group // rows)):
+            first, last = tile * rows, min((tile + 1) * rows, m * group) - 1
+            hi = length - m + last // group + 1
+            lo = max(length - m + first // group - window + 1, 0) if window else 0
+            steps = opening + (hi - 1) // keys - lo // keys + 1
+            total += p.heads * steps
+            longest = max(longest, steps)
+    return total / torch.cuda.get_device_properties(0).multi_processor_count, longest
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim,heads,group,page,window,counts", [
+    (128, 4, 4, 16, 0, [512] * 12), (64, 16, 1, 64, 0, [600] * 8), (128, 8, 2, 128, 300, [512, 700, 90, 640] * 3), (64, 2, 7, 32, 512, [700, 333, 64, 901] * 4)])
+def test_many_items_a_block(dtype, dim, heads, group, page, window, counts):
+    # a block goes from item to item: new queries, S and O used again, the rings of units and slots several times round
+    rng = np.random.default_rng(73)
+    new = counts
+    length = [m + int(rng.integers(0, 1100)) for m in new]
+    p = Paged(74, dtype, heads, dim, page, new, length)
+    share, longest = steps_a_share(p, group, window)
+    assert share > 1.5 * longest and share > 12
+    q, out, lse = attend(p, TYPES[dtype], heads * group, window=window)
+    for _ in range(3):
+        again, l = p.cache.attend(q, *p.tokens(), window=window, lse=True)
+        assert torch.equal(again, out) and torch.equal(l, lse)
+
+
+@pytest.mark.parametrize("store,dtype", [("e4m3", "bf16"), ("int8", "f16"), ("bf16", "bf16")])
+def test_blocks_and_single_tokens_of_many_requests(store, dtype):
+    rng = np.random.default_rng(75)
+    length = [int(v) for v in rng.integers(300, 4000, 48)]
+    p = Paged(76, store, 4, 128, 64, [int(v) for v in rng.integers(0, 9, 48)], length)
+    attend(p, TYPES[dtype], 16, max_new=8)
+
+
+# ---- layouts ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("store,dtype", [("bf16", "bf16"), ("f16", "f16"), ("e4m3", "bf16"), ("int8", "f16")])
+@pytest.mark.parametrize("page", [8, 16, 128])
+def test_pages_further_apart_than_their_size(store, dtype, page):
+    p = Paged(77, store, 2, 128, page, [1, 9, 130], [500, 9, 400])
+    own = p.cache
+    if page == 16:                                               # 16 bytes of something else between pages
+        gap, size = 16 // own.k.element_size(), own.k[0].numel()
+        far = [torch.zeros(p.pages * (size + gap), dtype=torch.uint8 if own.k.element_size() == 1 else torch.int16, device=DEV).view(own.k.dtype)
+               .as_strided(own.k.shape, (size + gap,) + own.k.stride()[1:]) for _ in range(2)]
+    else:                                                        # keys and values page by page in one allocation
+        both = torch.stack([own.k.view(torch.uint8), own.v.view(torch.uint8)], 1)
+        far = [both[:, i].view(own.k.dtype) for i in range(2)]
+    far[0].view(torch.uint8).copy_(own.k.view(torch.uint8))
+    far[1].view(torch.uint8).copy_(own.v.view(torch.uint8))
+    q, out, lse = attend(p, TYPES[dtype], 6)
+    p.cache = api.PagedCache(*far, *(s for s in (own.k_scale, own.v_scale) if s is not None))
+    got, l = p.cache.attend(q, *p.tokens(), lse=True)
+    assert torch.equal(got, out) and torch.equal(l, lse)
+    for a, b in zip(p.cache.read(*p.tokens(), sum(p.new)), own.read(*p.tokens(), sum(p.new))):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("store,dtype", [("bf16", "bf16"), ("int8", "f16")])
+def test_a_table_with_rows_of_its_own_stride(store, dtype):
+    p = Paged(78, store, 2, 64, 16, [1, 9, 130], [500, 9, 400])
+    q, out, lse = attend(p, TYPES[dtype], 6)
+    wide = torch.full((len(p.new), p.d_table.shape[1] + 5), 10 ** 6, dtype=torch.int32, device=DEV)
+    table = wide[:, :p.d_table.shape[1]]
+    table.copy_(p.d_table)
+    t = p.tokens()[:2] + (table,)
+    got, l = p.cache.attend(q, *t, lse=True)
+    assert torch.equal(got, out) and torch.equal(l, lse)
+    for a, b in zip(p.cache.read(*t, sum(p.new)), p.cache.read(*p.tokens(), sum(p.new))):
+        assert torch.equal(a, b)
+    before = [x.clone() for x in p.cache.read(*p.tokens(), sum(p.new))]
+    kv = torch.randn(sum(p.new), 2, 2, 64, device=DEV).bfloat16()
+    p.cache.write(kv[:, 0], kv[:, 1], *t)
+    after = p.cache.read(*p.tokens(), sum(p.new))
+    p.cache.write(kv[:, 0], kv[:, 1], *p.tokens())
+    again = p.cache.read(*p.tokens(), sum(p.new))
+    assert all(torch.equal(a, b) and not torch.equal(a, c) for a, b, c in zip(after, again, before))
+
+
+@pytest.mark.parametrize("store,dtype", [("bf16", "bf16"), ("f16", "f16"), ("e4m3", "f16")])
+@pytest.mark.parametrize("page", [512, 4096])
+def test_large_pages(store, dtype, page):
+    p = Paged(79, store, 2, 64, page, [1, 9, 200], [5000, 9, 700], stray_pages=1)
+    attend(p, TYPES[dtype], 4)
+    k, v = p.cache.read(prefix(p.length), p.lengths, p.d_table, sum(p.length), dtype=torch.float32)
+    want = [torch.from_numpy(np.concatenate([p.rows(b)[i] for b in range(3)])).to(DEV) for i in range(2)]
+    assert torch.equal(k, want[0].float()) and torch.equal(v, want[1].float())
+
+
+@pytest.mark.parametrize("most", [1, 3, 20])
+def test_more_new_tokens_than_the_hint_says(most):
+    p = Paged(80, "bf16", 2, 128, 16, [300, 1, 40, 17], [900, 200, 40, 300])
+    attend(p, torch.bfloat16, 8, max_new=most)
+    attend(p, torch.bfloat16, 8, max_new=most, window=100)
 
 
 # ---- offsets that reach past the call's rows ----------------------------------------------------------------------------
@@ -250,3 +373,29 @@ def test_blocks_with_a_tile_and_without_a_second_one(dtype, new, length, heads, 
     times[1].record()
     torch.cuda.synchronize()
     assert all(torch.equal(g, out) for g in got) and times[0].elapsed_time(times[1]) < 50 * 5
+
+
+# ---- from the pruning into the cache ------------------------------------------------------------------------------------
+
+def test_the_kept_tokens_of_a_selection_go_into_the_cache():
+    wl = workloads.make_workload("kept", seed=82, dtype=torch.bfloat16, batch=3, n_vis=(150, 700), n_txt=(3, 20), d=256, n_heads=2, rank=16,
+                                 keep_ratio=0.25).to(DEV)
+    pruner = api.Pruner.for_workload(wl)
+    m = pruner.marshal(wl)
+    keep_idx, ko, *_ = pruner.select(m, pruner.score(m)[2])
+    kept = [int(v) for v in np.diff(ko)]
+    kv = torch.randn(2, wl.total_vis, 4, 128, device=DEV).bfloat16()
+    dense = [pruner.compact_rows(m, keep_idx, ko, x) for x in kv]
+    pruner.close()
+    got = []
+    for direct in (True, False):
+        p = Paged(83, "e4m3", 4, 128, 16, kept, kept, fill=False)
+        if direct:
+            p.cache.write(kv[0], kv[1], *p.tokens(), rows=keep_idx, row_offsets=i32(wl.vis_offsets.tolist()))
+        else:
+            p.cache.write(*dense, *p.tokens())
+        got.append(p.cache.read(*p.tokens(), sum(kept)))
+        q = torch.randn(sum(kept), 8, 128, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)).bfloat16()
+        out, lse = p.cache.attend(q, *p.tokens(), lse=True)
+        check(p, q, out, lse, 128 ** -0.5)
+    assert all(torch.equal(a, b) and a.isfinite().all() for a, b in zip(*got))
