@@ -286,7 +286,8 @@ PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (scale == -1.0 && PyErr_Occurred()) return nullptr;
   if (!int_arg(a[2], size) || !int_arg(a[8], window) || !int_arg(a[9], most)) return nullptr;
   if (!is_int(window) || !is_int(most)) Py_RETURN_NONE;
-  const bool logs = PyObject_IsTrue(a[10]) == 1;
+  const int logs = PyObject_IsTrue(a[10]);
+  if (logs < 0) return nullptr;
   at::Tensor out;
   if (a[11] == Py_None) {
     out = at::empty({q.size(0), q.size(1), q.size(2)}, q.options());

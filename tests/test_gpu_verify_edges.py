@@ -399,3 +399,12 @@ def test_the_kept_tokens_of_a_selection_go_into_the_cache():
         out, lse = p.cache.attend(q, *p.tokens(), lse=True)
         check(p, q, out, lse, 128 ** -0.5)
     assert all(torch.equal(a, b) and a.isfinite().all() for a, b in zip(*got))
+
+
+def test_an_argument_without_a_truth_value_is_refused():
+    p = Paged(88, "bf16", 2, 64, 16, [3], [20])
+    q = torch.randn(3, 4, 64, device=DEV).bfloat16()
+    with pytest.raises(ValueError):                              # what bool() says of it
+        p.cache.attend(q, *p.tokens(), lse=np.array([1, 2]))
+    out, lse = p.cache.attend(q, *p.tokens(), lse=np.True_)
+    check(p, q, out, lse, 0.125)
