@@ -281,8 +281,10 @@ int covspec_cache_read(const covspec_cache* cache, const covspec_tokens* tokens,
 
 /* Attention of the call's tokens over the cache, which already holds them (covspec_cache_write).  The token at position p
  * attends to the positions max(0, p - window + 1) .. p of its request: o = sum_j softmax_j(scale q . k_j) v_j.  Query head h
- * reads key head h / (q_heads / heads).  Probabilities are rounded to dtype before the second product; scores, maxima, sums and
- * accumulators are float32.  A token without a key (a position below 0) gets zeros and the sum -inf.  What the pages hold past
+ * reads key head h / (q_heads / heads).  Scores, maxima, sums and accumulators are float32.  Probabilities are rounded to dtype before
+ * the second product.  With an 8-bit store the products are float16 whatever dtype is: what is rounded is the probability times the
+ * value's scale, by half a step of float16 or of 2^-38 of the largest such term at hand; and bfloat16 queries are brought to float16 by a
+ * power of two for each row, exactly but for elements 2^-29 times as small as the row's largest.  A token without a key (a position below 0) gets zeros and the sum -inf.  What the pages hold past
  * a request's length, or before every window of the call, does not matter, whatever it is; the values at positions that one of a
  * request's new tokens sees and another does not have to be finite, or both may become NaN.
  *  dtype         of q and out: COVSPEC_BF16 or COVSPEC_F16; the cache's store is the same or an 8-bit one

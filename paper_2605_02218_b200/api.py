@@ -624,7 +624,8 @@ def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, device: torch.device, 
 class PagedCache:
     """Keys and values of one layer in pages (covspec_cache): `k`, `v` [pages, heads, page_size, head_dim] in float32,
     bfloat16, float16, float8_e4m3fn or int8, each page dense; the two 8-bit types come with `k_scale`, `v_scale` [pages, heads,
-    page_size] float32.  The tensors stay the caller's: `k` and `v` may be views of one allocation.
+    page_size] float32.  The tensors stay the caller's: `k` and `v` may be views of one allocation.  A float32 cache is written
+    and read only.  Results carry no gradient.
 
     The calls take the tokens of a batch, packed request by request: `offsets` [batch + 1], `lengths` [batch] and `table` [batch,
     pages of a request], int32 on the cache's device.  Request b's tokens offsets[b] .. offsets[b+1] are the last ones of its
@@ -798,7 +799,8 @@ def edit_logits(z: torch.Tensor, row_offsets: torch.Tensor, *, history: Optional
     drafted blocks, before `correct` or `branch_candidates`.  `row_offsets` [batch + 1] delimits the requests' rows; row j of a
     request counts the tokens `drafted` at its rows before j as history.  `mask`: int32 [rows, ceil(vocab / 32)], bit w % 32 of
     word w / 32 allows token w.  Everything on z's device, ids and offsets int32, factors float32.  Returns the edited logits (in
-    `out` if given, which may be z); rows of no request and columns past the vocabulary are undefined, or left as they were."""
+    `out` if given, which may be z), without a gradient; rows of no request and columns past the vocabulary are undefined, or left as
+    they were."""
     lib = _lib or load_library()
     if _native is not None:
         got = _native.edit_logits(z, row_offsets, history, history_offsets, prompt_lengths, drafted, repetition, presence, frequency,

@@ -43,8 +43,8 @@ constexpr uint32_t kPolls = 1u << 18;
 // A wait of the whole warp: its lanes poll together and leave together.  And every lane itself arrives at the barrier without which the one
 // that it waits for does not complete again, so that no lane can be left behind by two phases, whatever the compiler makes of the
 // warp's convergence: with a loop of its own for each lane, a vote behind it and arrivals by lane 0, lanes left one by one, and in some
-// builds lane 0 went on alone and the others waited for a phase that was over.  (One lane that polls for all: 202 us for 142 with 64 single
-// tokens over e4m3 caches.)
+// builds lane 0 went on alone and the others waited for a phase that was over.  (One lane that polls for all: 202 us for 138 with 64 single
+// tokens over e4m3 caches, 975 for 680 with prompts.)
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint32_t polls) {
   for (uint32_t i = 0; i < polls; ++i) {
     if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar, parity))) return true;

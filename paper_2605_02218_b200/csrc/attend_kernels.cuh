@@ -8,9 +8,9 @@
 // unit to unit each at its own pace and meet at the end of an item only.
 //
 // Measured (reading the cache once is the floor): 64 single tokens over e4m3 caches of 500-16384 positions, 32 query heads on 8 of 128:
-// 142 us, 4.1 TB/s; blocks of 8 tokens over 32 bf16 caches of 300-4096, 28 heads on 4: 44 us, 2.0 TB/s; 24 prompt chunks of up to 700
-// tokens over int8 caches, 14 heads on 2 of 64, window 1024: 326 us.  Bound by the chain of instructions of a warp from unit to unit
-// (eight computing warps an SM; issue slots 42 % busy, HBM 36 % in the first of these at 200 us), the last one by mma.sync's rate.
+// 138 us, 4.2 TB/s; blocks of 8 tokens over 32 bf16 caches of 300-4096, 28 heads on 4: 44 us, 2.0 TB/s; 24 prompt chunks of up to 700
+// tokens over int8 caches, 14 heads on 2 of 64, window 1024: 321 us.  Bound by the chain of instructions of a warp from unit to unit
+// (eight computing warps an SM; issue slots 40 % busy, HBM 50 % in the first of these), the last one by mma.sync's rate.
 //
 // 8-bit rows are exact in float16, so their scales stay outside the products: s_ij = (q_i . k_j) * key scale, and the probability
 // takes the value's scale before it is rounded to 16 bits.  So that it cannot leave float16's range, the running maximum is the
@@ -25,7 +25,9 @@ namespace covspec {
 namespace attend {
 
 constexpr int kThreads = 160, kWarps = 4;        // threads of a CTA; its warps that compute
-constexpr int kOpen = 2;                         // units that beginning and ending an item costs (none: shares end up to 15 % apart)
+// Units that beginning and ending an item costs.  Without: 155 us for 138 with 64 single tokens over e4m3 caches, 45.2 for 44.0 with blocks
+// of 8 tokens, 12.0 for 12.5 with one token over 900 positions (the share's units are counted item by item).
+constexpr int kOpen = 2;
 
 template <int STORE, int DIM, int ROWS> struct Layout {
   static constexpr bool k8 = STORE >= cache::kE4M3;

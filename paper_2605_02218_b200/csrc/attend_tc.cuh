@@ -5,21 +5,23 @@
 // tiles; the probabilities overwrite S in 16 bits and are the A operand of the second product from there.  Keys are K-major, values
 // MN-major (keys are the inner dimension of the second product), both as rows of 64 features in 128-byte swizzled tiles.
 //
-// Warps: 0-7 and 8-15 softmax of tile 0 and 1, a row of it two threads in two warps, each half of a unit's keys; 16 issues the
-// products; 17-19 bring queries, and 17 keys and values, into shared memory: tiled copies, a box as many rows as a page has (at most
+// Warps: 0-7 and 8-15 softmax of tile 0 and 1, a row of it two threads in two warps, each half of a unit's keys; a thread of 16
+// issues the products (with its warp's other lanes waiting along: 655 us for 668 in the case below, but they arrive nowhere and so could
+// be left behind at a wait); 17-19 bring queries, and 17 keys and values, into shared memory: tiled copies, a box as many rows as a page has (at most
 // 128), a box a lane.  Where not every key of a unit is there, the values' other rows are cleared before the products may see them.
 //
 // The running maximum is only a reference that keeps the exponentials in range: a row keeps it
 // while a unit's probabilities add up to at most 2^14, so that O is rescaled seldom and one pass over S makes the probabilities.  A
 // warp with a row beyond that goes over S again with new references.
 //
-// 16-bit caches only: 8-bit rows would have to be widened into shared memory first, and the form of this kernel that did so stood still
-// on a large call for a reason that was not found; they take the kernel for few rows.
+// 16-bit caches only: 8-bit rows would have to be widened into shared memory first.  The form of this kernel that did so stood still on a
+// large call; its waits were of the kind that warp_wait (attend_common.cuh) says of what happened to them.  8-bit caches take the kernel
+// for few rows.
 //
-// Measured: 8 prompts of 2048 tokens over caches of 2048-4096, 32 heads on 8 of 128, bf16: 600-680 us, 0.72-0.8 PFLOP/s (with mma.sync
-// 2756).  A unit takes about 3700 cycles: 2330 of products (16 of 128 x 128 x 16 for each of the two factors; the two tiles' operands
-// take all of shared memory's bandwidth), in the rest the products wait for probabilities: 32768 exponentials are 2048 cycles of the
-// special-function units, and the two tiles overlap in part only.
+// Measured: 8 prompts of 2048 tokens over caches of 2048-4096, 32 heads on 8 of 128, bf16: 665-690 us, 0.71-0.73 PFLOP/s (with mma.sync
+// 2756).  An SM has 204 units and takes 5200 cycles for one, beginnings and ends of items included: 2330 of products (16 of 128 x 128 x 16
+// for each of the two factors; the two tiles' operands take all of shared memory's bandwidth), in the rest the products wait for
+// probabilities: 32768 exponentials are 2048 cycles of the special-function units, and the two tiles overlap in part only.
 #pragma once
 #include "attend_call.cuh"
 #include "attend_kernels.cuh"
@@ -33,7 +35,7 @@ using namespace tc;
 constexpr int kRows = kWideRows, kKeys = kWideKeys;
 constexpr int kThreads = 20 * 32, kSoftmaxWarps = 16;
 constexpr int kCopyWarps = 3, kProducers = kCopyWarps * 32;
-constexpr int kOpen = 4;                    // units that beginning and ending an item costs (8 prompts of 2048 tokens: 688 us without, 604)
+constexpr int kOpen = 4;                    // units that beginning and ending an item costs (8 prompts of 2048 tokens: 740 us without, 685)
 constexpr float kMost = 16384.f;            // a unit's probabilities add up to no more over their reference
 
 template <int STORE, int DIM> struct Layout {
