@@ -65,12 +65,12 @@ struct Request {
 };
 __device__ __forceinline__ Request load_request(const Params& p, int b) {
   Request r;
-  const int a = p.t.offsets[b], e = p.t.offsets[b + 1];
   const int length = max(p.t.lengths[b], 0);
-  r.q0 = max(a, 0);
+  r.q0 = max(p.t.offsets[b], 0);
+  const int e = max(p.t.offsets[b + 1], r.q0);         // no end so far before the start that the difference leaves 32 bits
   // a token keeps its position where its request begins before the call's rows or ends behind them; a call has fewer than 2^30 tokens,
   // so what lies further below 0 stays there
-  r.first = max(length - max(e - r.q0, 0), -(1 << 30));
+  r.first = max(length - (e - r.q0), -(1 << 30));
   r.keys = (int)min((long long)length, (long long)p.t.width << p.c.page_shift);
   r.rows = max(min(e, p.n) - r.q0, 0) * p.group;
   if (r.rows <= p.rows_over || r.rows > p.rows_upto) r.rows = 0;

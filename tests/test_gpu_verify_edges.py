@@ -375,6 +375,18 @@ def test_blocks_with_a_tile_and_without_a_second_one(dtype, new, length, heads, 
     assert all(torch.equal(g, out) for g in got) and times[0].elapsed_time(times[1]) < 50 * 5
 
 
+@pytest.mark.parametrize("store,dtype", [("bf16", "bf16"), ("int8", "f16")])
+@pytest.mark.parametrize("end", [-2 ** 31, -2 ** 31 + 3, -2 ** 31 + 100, -1, 0, 99])
+def test_an_end_before_the_start_is_a_request_without_rows(store, dtype, end):
+    # in 32 bits the least number less the start is a large one
+    p = Paged(89, store, 2, 64, 16, [100, 0, 0], [150, 200, 30])
+    q = torch.randn(120, 4, 64, device=DEV).to(TYPES[dtype])
+    out = torch.full_like(q, 3.0)
+    p.cache.attend(q, i32([0, 100, end, end]), p.lengths, p.d_table, out=out)
+    assert (out[100:] == 3).all()
+    check(p, q[:100], out[:100], None, 0.125)
+
+
 # ---- from the pruning into the cache ------------------------------------------------------------------------------------
 
 def test_the_kept_tokens_of_a_selection_go_into_the_cache():
